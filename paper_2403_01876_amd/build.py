@@ -5,6 +5,8 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -25,12 +27,20 @@ def _run(cmd):
     subprocess.run(cmd, check=True)
 
 
+SOURCES = ("dv_attend.hip", "dv_kernels.hip", "dv_api.cpp", "dv_swapper.cpp", "dv_streamer.cpp",
+           "dv_noalloc.hip", "dv_attn.cpp", "dv_quant.hip", "dv_evict.hip")
+
+
 def build_libdv(out: str = LIBDV, flags=()) -> str:
-    srcs = [os.path.join(PKG, "csrc", f) for f in ("dv_kernels.hip", "dv_api.cpp",
-                                                    "dv_swapper.cpp", "dv_streamer.cpp",
-                                                    "dv_noalloc.hip")]
-    tmp = out + ".tmp"
-    _run([HIPCC, *HIP_FLAGS, *flags, "-x", "hip", *srcs, "-o", tmp])
+    """One object per source, compiled side by side, then linked."""
+    with tempfile.TemporaryDirectory(dir=os.path.dirname(out)) as d:
+        objs = [os.path.join(d, f + ".o") for f in SOURCES]
+        with ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as pool:
+            list(pool.map(lambda so: _run([HIPCC, *HIP_FLAGS, *flags, "-c", "-x", "hip",
+                                           os.path.join(PKG, "csrc", so[0]), "-o", so[1]]),
+                          zip(SOURCES, objs)))
+        tmp = out + ".tmp"
+        _run([HIPCC, *HIP_FLAGS, *objs, "-o", tmp])
     os.replace(tmp, out)
     return out
 

@@ -1,0 +1,1032 @@
+// Attention over an 8-bit cache: e4m3 codes, a power-of-two scale per block.
+//
+// Codes become f16 or bf16 (the queries' type) as they enter the matrix units:
+// the conversion multiplies by the scale, and code * 2^e is exact in both types
+// within their range, so neither keys nor values are rounded a second time.
+// Scores come out transposed, S^T = K Q^T, tokens down and queries across: a
+// lane then holds several tokens of one query, which is how the second product,
+// O^T = V^T P^T, wants its right operand, so probabilities never leave their
+// registers.  (The order of tokens along that product's inner axis is free as
+// long as V follows it.)
+//
+// Softmax runs in one pass in powers of two: s2 = score * log2(e), a reference m
+// per query and sums relative to it.  m is set kLift below the largest score and
+// moves only when a score exceeds that by more than 8, so the common step needs no
+// exchange between lanes and no rescaling; probabilities then reach 2^(8 + kLift)
+// at most, which costs no precision.  kLift is 7 for f16, whose probabilities stay
+// normal numbers down to 2^-21 of the largest so (a value 2^12 times another's
+// shows their rounding below 2^-14 otherwise), and 0 for bf16.
+#include "dv_attn_internal.h"
+
+namespace dv {
+namespace {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLow = -1e30f;  // "no score yet"; a hidden score is -infinity
+constexpr float kLn2 = 0.69314718055994531f, kLog2e = 1.4426950408889634f;
+constexpr float kSlack = 8.f;
+
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+template <bool BF16>
+struct Ty;
+template <>
+struct Ty<false> {
+  static constexpr uint32_t kInf = 0x7c00, kOne = 0x3c00;
+  static constexpr float kLift = 7.f;
+  // bytes 0, 1 (or 2, 3) of w, times the scale
+  template <bool HI>
+  static __device__ __forceinline__ uint32_t cvt(uint32_t w, float s) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, s, HI));
+  }
+  static __device__ __forceinline__ uint32_t pack(float a, float b) {
+    return __builtin_bit_cast(uint32_t, f16x2{(_Float16)a, (_Float16)b});
+  }
+  static __device__ __forceinline__ float lo(uint32_t w) {
+    return (float)__builtin_bit_cast(f16x2, w)[0];
+  }
+  static __device__ __forceinline__ float hi(uint32_t w) {
+    return (float)__builtin_bit_cast(f16x2, w)[1];
+  }
+  static __device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a),
+                                                  __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ f32x16 mma32(u32x4 a, u32x4 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a),
+                                                  __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  }
+};
+template <>
+struct Ty<true> {
+  static constexpr uint32_t kInf = 0x7f80, kOne = 0x3f80;
+  static constexpr float kLift = 0.f;
+  template <bool HI>
+  static __device__ __forceinline__ uint32_t cvt(uint32_t w, float s) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, HI));
+  }
+  static __device__ __forceinline__ uint32_t pack(float a, float b) {
+    return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
+  }
+  static __device__ __forceinline__ float lo(uint32_t w) { return __uint_as_float(w << 16); }
+  static __device__ __forceinline__ float hi(uint32_t w) {
+    return __uint_as_float(w & 0xffff0000u);
+  }
+  static __device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
+                                                   __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ f32x16 mma32(u32x4 a, u32x4 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                   __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  }
+};
+
+// The sequence that holds work item `item` (as find_seq of the streaming
+// kernels: the count of first items at or below it names it).
+__device__ __forceinline__ int seq_of(const AttendArgs& a, int item) {
+  const int lane = threadIdx.x & 63;
+  int below = 0;
+  for (int i = 0; i < a.nseq; i += 64) below += __popcll(__ballot(a.item[i + lane] <= item));
+  return __builtin_amdgcn_readfirstlane(below - 1);
+}
+
+// Called on products' results before any branch: ends the wait for them in the
+// block of the products.  Left to itself, the compiler (ROCm 7.2) counts the wait
+// states between a product and the first read of its result along one path only
+// where an `if` without `else` comes between, and read the last register too
+// early on the path that skips it.
+template <typename V>
+__device__ __forceinline__ void settle(V& a) {
+  asm volatile("s_nop 12" : "+v"(a));
+}
+
+// 0x80 in each byte of w that is a NaN code.
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
+  return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+}
+
+// Halves 0 (or 1) of two words, a's below b's.
+__device__ __forceinline__ uint32_t lows(uint32_t a, uint32_t b) {
+  return __builtin_amdgcn_perm(b, a, 0x05040100u);
+}
+__device__ __forceinline__ uint32_t highs(uint32_t a, uint32_t b) {
+  return __builtin_amdgcn_perm(b, a, 0x07060302u);
+}
+
+// ---------------------------------------------------------------------------
+// Few rows (decode steps): a workgroup takes a chunk of one head's tokens, its
+// four waves 32 tokens at a time in turn; 16x16x32 products, queries in RT tiles
+// of 16 columns.  Keys go from memory to the matrix unit in the order they are
+// stored: lane (token l % 16, group l / 16) takes 16 bytes of its token's row.
+// Values: lane (dims (l % 16) * Dp / 16 ..., group g) takes its dims of eight
+// tokens, and the 8 x 8 transposition that the product needs happens in its own
+// registers.  Nothing of the cache passes through LDS.
+// Bound by HBM.
+// ---------------------------------------------------------------------------
+template <bool BF16, int DP, int RT>
+__global__ void __launch_bounds__(kThreads) attend_split_kernel(AttendArgs a, int direct) {
+  using T = Ty<BF16>;
+  constexpr int KL = DP / 64, VW = DP / 64, KS = DP / 32, OJ = DP / 16;
+  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+  const QLayout& q = a.q;
+  const int tid = threadIdx.x, wave = tid >> 6, l = tid & 63, c = l & 15, g = l >> 4;
+
+  const int item = blockIdx.x, b = seq_of(a, item), sb = a.b0 + b;
+  const int len = a.len[b], nq = a.tok[b + 1] - a.tok[b], rows = nq * a.G;
+  const int nsplit = max(1, (len + a.chunk - 1) / a.chunk);
+  const int k = item - a.item[b], h = k / nsplit, c0 = (k - h * nsplit) * a.chunk;
+  const int cn = min(a.chunk, len - c0);  // tokens of this chunk
+
+  uint32_t* off = (uint32_t*)lds;         // each token's row, in 16 bytes from the head's base
+  float* ks = (float*)lds + a.chunk;      // scales; 0: an unmapped block
+  float* vs = (float*)lds + 2 * a.chunk;
+  float* pos = (float*)lds + 3 * a.chunk;
+  const int64_t slab = 2 * (int64_t)a.layer;
+  const uint8_t* kb = q.codes + slab * q.s_slab + sb * q.s_b + h * q.s_h;
+  const uint8_t* vb = kb + q.s_slab;
+  const float* sk = q.scale + slab * q.c_slab + sb * q.c_b + h * q.c_h;
+  const int64_t slots = (((int64_t)a.layer * q.batch + sb) * q.heads + h) * (int64_t)q.cap;
+  int bad = 0;
+  for (int i = tid; i < ((cn + kSplitStep - 1) & -kSplitStep); i += kThreads) {
+    const int t = min(c0 + i, len - 1), j = q.d_bs.div(t);
+    int64_t blk = j;
+    bool hole = false;
+    if (q.bt) {
+      blk = q.bt[(int64_t)sb * q.max_blocks + j];
+      hole = (uint64_t)blk >= (uint64_t)q.num_blocks;
+      blk = hole ? 0 : blk;
+    }
+    off[i] = (uint32_t)((blk * q.s_blk + (int64_t)(t - j * q.bs) * q.D) >> 4);
+    ks[i] = hole ? 0.f : sk[blk * q.c_blk];
+    vs[i] = sk[blk * q.c_blk + q.c_slab];
+    if (a.slopes) pos[i] = (float)(q.position ? q.position[slots + t] : t);
+    bad |= hole;
+  }
+
+  // The queries, and what each column (row c of tile rt) may see.
+  u32x4 qr[RT][KS];
+  int limit[RT];
+  float slope[RT], here[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int r = rt * 16 + c, i = r / a.G, head = h * a.G + (r - i * a.G);
+    const bool on = r < rows;
+    const uint16_t* src = (const uint16_t*)a.query +
+                          (int64_t)(on ? a.tok[b] + i : 0) * a.q_token + (int64_t)head * a.q_head;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const int d = (s >> 1) * 64 + g * 16 + (s & 1) * 8;
+      qr[rt][s] = on && d < q.D ? *(const u32x4*)(src + d) : u32x4{0, 0, 0, 0};
+    }
+    limit[rt] = on ? len - nq + i : -1;
+    slope[rt] = here[rt] = 0.f;
+    if (a.slopes && on && limit[rt] >= 0) {
+      slope[rt] = a.slopes[head] * kLog2e;
+      here[rt] = (float)(q.position ? q.position[slots + limit[rt]] : limit[rt]);
+    }
+  }
+  const bool holes = __syncthreads_or(bad);
+  const int all_see = len - nq;  // slots up to this one are seen by every row
+
+  const int kd = g * 16, vd = c * (DP / 16);
+  const bool pad = q.D < DP;
+  struct Tile {
+    u32x4 k[2][KL];
+    uint32_t v[8][VW];
+  };
+  auto load = [&](Tile& x, int t) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const uint8_t* p = kb + (uint64_t)off[t + u * 16 + c] * 16;
+#pragma unroll
+      for (int i = 0; i < KL; ++i)
+        x.k[u][i] = *(const u32x4*)(p + (pad && kd + 64 * i >= q.D ? 0 : kd + 64 * i));
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const u32x4 o = *(const u32x4*)(off + t + u * 16 + g * 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint8_t* p = vb + (uint64_t)o[i] * 16 + (pad && vd >= q.D ? 0 : vd);
+        if constexpr (VW == 1) x.v[u * 4 + i][0] = *(const uint32_t*)p;
+        if constexpr (VW == 2) {
+          const u32x2 w = *(const u32x2*)p;
+          x.v[u * 4 + i][0] = w[0];
+          x.v[u * 4 + i][1] = w[1];
+        }
+        if constexpr (VW == 4) {
+          const u32x4 w = *(const u32x4*)p;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x.v[u * 4 + i][e] = w[e];
+        }
+      }
+    }
+  };
+
+  f32x4 o[RT][OJ];
+  float m[RT], sum[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    m[rt] = kLow;
+    sum[rt] = 0.f;
+#pragma unroll
+    for (int j = 0; j < OJ; ++j) o[rt][j] = f32x4{0, 0, 0, 0};
+  }
+  const int64_t pitch = (len + 31) & ~31;
+  float* sc = a.scores + (int64_t)a.soff[b] * 32 + (int64_t)h * rows * pitch;
+
+  auto compute = [&](Tile& x, int t) {
+    f32x4 s[RT][2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const float scale = ks[t + u * 16 + c];
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) s[rt][u] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < KL; ++i) {
+        u32x4 w = x.k[u][i];
+        if (pad && kd + 64 * i >= q.D) w = u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const u32x4 y = {T::template cvt<false>(w[2 * e], scale),
+                           T::template cvt<true>(w[2 * e], scale),
+                           T::template cvt<false>(w[2 * e + 1], scale),
+                           T::template cvt<true>(w[2 * e + 1], scale)};
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt)
+            s[rt][u] = T::mma16(y, qr[rt][2 * i + e], s[rt][u]);
+        }
+      }
+    }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      settle(s[rt][0]);
+      settle(s[rt][1]);
+    }
+    const int first = c0 + t + g * 4;  // this lane's tokens: first + 16 u + r
+    const bool mask = holes || c0 + t + kSplitStep - 1 > all_see;
+    uint32_t seen[RT];  // bit u * 4 + r
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) s[rt][u] = s[rt][u] * a.scale2;
+      if (a.slopes) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const f32x4 at = *(const f32x4*)(pos + t + u * 16 + g * 4);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) s[rt][u][r] += slope[rt] * (at[r] - here[rt]);
+        }
+      }
+      if (mask) {
+        seen[rt] = 0;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const f32x4 there = *(const f32x4*)(ks + t + u * 16 + g * 4);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const bool sees = first + u * 16 + r <= limit[rt] && there[r] != 0.f;
+            s[rt][u][r] = sees ? s[rt][u][r] : -INFINITY;
+            seen[rt] |= (uint32_t)sees << (u * 4 + r);
+          }
+        }
+      }
+      if (a.weigh && rt * 16 + c < rows) {
+        float* to = sc + (int64_t)(rt * 16 + c) * pitch + first;
+        *(f32x4*)to = s[rt][0];
+        *(f32x4*)(to + 16) = s[rt][1];
+      }
+      float most = s[rt][0][0];
+#pragma unroll
+      for (int i = 1; i < 8; ++i) most = fmaxf(most, s[rt][i >> 2][i & 3]);
+      if (__any(most > m[rt] + (kSlack + T::kLift))) {
+        float up = fmaxf(most - T::kLift, m[rt]);
+        up = fmaxf(up, __shfl_xor(up, 16));
+        up = fmaxf(up, __shfl_xor(up, 32));
+        const float f = exp2_(m[rt] - up);
+        m[rt] = up;
+        sum[rt] *= f;
+#pragma unroll
+        for (int j = 0; j < OJ; ++j) o[rt][j] = o[rt][j] * f;
+      }
+    }
+    // Probabilities as the sum of two 16-bit numbers: the matrix unit has time
+    // to spare here, and the results keep 32-bit accuracy.
+    u32x4 hi[RT], lo[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float p0 = exp2_(s[rt][i >> 1][(2 * i) & 3] - m[rt]);
+        const float p1 = exp2_(s[rt][i >> 1][(2 * i + 1) & 3] - m[rt]);
+        sum[rt] += p0 + p1;
+        hi[rt][i] = T::pack(p0, p1);
+        lo[rt][i] = T::pack(p0 - T::lo(hi[rt][i]), p1 - T::hi(hi[rt][i]));
+      }
+    }
+    if (mask) {
+      // A NaN value reaches the queries that see its token and no others: it
+      // leaves the product below, and where a product of "is NaN" and "is seen"
+      // is not zero the result is NaN.
+      uint32_t any = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int w = 0; w < VW; ++w) any |= nan_bytes(x.v[i][w]);
+      if (__any(any != 0)) {
+#pragma unroll
+        for (int w = 0; w < VW; ++w) {
+          uint32_t is[8][2];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const uint32_t n = nan_bytes(x.v[i][w]) >> 7;
+            is[i][0] = (n & 1) * T::kOne | ((n >> 8) & 1) * (T::kOne << 16);
+            is[i][1] = ((n >> 16) & 1) * T::kOne | ((n >> 24) & 1) * (T::kOne << 16);
+            x.v[i][w] &= ~(n * 0xffu);
+          }
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) {
+            u32x4 sees;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              sees[i] = ((seen[rt] >> (2 * i)) & 1) * T::kOne |
+                        ((seen[rt] >> (2 * i + 1)) & 1) * (T::kOne << 16);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              u32x4 y;
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                y[i] = e & 1 ? highs(is[2 * i][e >> 1], is[2 * i + 1][e >> 1])
+                             : lows(is[2 * i][e >> 1], is[2 * i + 1][e >> 1]);
+              const f32x4 z = T::mma16(y, sees, f32x4{0, 0, 0, 0});
+#pragma unroll
+              for (int r = 0; r < 4; ++r)
+                o[rt][4 * w + e][r] = z[r] > 0.f ? NAN : o[rt][4 * w + e][r];
+            }
+          }
+        }
+      }
+    }
+    float scale[8];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const f32x4 w = *(const f32x4*)(vs + t + u * 16 + g * 4);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) scale[u * 4 + r] = w[r];
+    }
+#pragma unroll
+    for (int w = 0; w < VW; ++w) {
+      uint32_t y[8][2];  // dims 0, 1 and 2, 3 of the word, for each token
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        y[i][0] = T::template cvt<false>(x.v[i][w], scale[i]);
+        y[i][1] = T::template cvt<true>(x.v[i][w], scale[i]);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        u32x4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          v[i] = e & 1 ? highs(y[2 * i][e >> 1], y[2 * i + 1][e >> 1])
+                       : lows(y[2 * i][e >> 1], y[2 * i + 1][e >> 1]);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          o[rt][4 * w + e] = T::mma16(v, hi[rt], o[rt][4 * w + e]);
+          o[rt][4 * w + e] = T::mma16(v, lo[rt], o[rt][4 * w + e]);
+        }
+      }
+    }
+  };
+
+  Tile x, y;
+  int t = wave * kSplitStep;
+  if (t < cn) load(x, t);
+  for (; t < cn; t += 2 * kSplitRound) {
+    if (t + kSplitRound < cn) load(y, t + kSplitRound);
+    compute(x, t);
+    if (t + kSplitRound < cn) {
+      if (t + 2 * kSplitRound < cn) load(x, t + 2 * kSplitRound);
+      compute(y, t + kSplitRound);
+    }
+  }
+
+  // Join the four waves.
+  __syncthreads();  // the tables are done with
+  float* sums = (float*)lds;                      // [wave][16][DP]
+  float* mls = sums + 4 * 16 * DP;                // [wave][RT * 16][2]
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    sum[rt] += __shfl_xor(sum[rt], 16);
+    sum[rt] += __shfl_xor(sum[rt], 32);
+    if (g == 0) {
+      mls[(wave * RT * 16 + rt * 16 + c) * 2] = m[rt];
+      mls[(wave * RT * 16 + rt * 16 + c) * 2 + 1] = sum[rt];
+    }
+  }
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    __syncthreads();
+    if (rt * 16 >= rows) break;
+    float most = kLow;
+    for (int w = 0; w < 4; ++w) most = fmaxf(most, mls[(w * RT * 16 + rt * 16 + c) * 2]);
+    const float f = exp2_(m[rt] - most);
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int j = 0; j < OJ; j += 4)
+        *(f32x4*)(sums + (wave * 16 + c) * DP + (g * 4 + r) * OJ + j) =
+            f32x4{o[rt][j][r] * f, o[rt][j + 1][r] * f, o[rt][j + 2][r] * f, o[rt][j + 3][r] * f};
+    __syncthreads();
+    for (int e = tid * 4; e < 16 * DP; e += kThreads * 4) {
+      const int rr = e / DP, d = e % DP, r = rt * 16 + rr;
+      if (r >= rows) continue;
+      f32x4 v = *(const f32x4*)(sums + e);
+#pragma unroll
+      for (int w = 1; w < 4; ++w) v += *(const f32x4*)(sums + w * 16 * DP + e);
+      float top = kLow, total = 0.f;
+      for (int w = 0; w < 4; ++w) top = fmaxf(top, mls[(w * RT * 16 + r) * 2]);
+      for (int w = 0; w < 4; ++w)
+        total += mls[(w * RT * 16 + r) * 2 + 1] * exp2_(mls[(w * RT * 16 + r) * 2] - top);
+      if (!direct) {
+        *(f32x4*)(a.part + ((int64_t)item * RT * 16 + r) * DP + d) = v;
+        if (d == 0) {
+          a.ml[((int64_t)item * RT * 16 + r) * 2] = top;
+          a.ml[((int64_t)item * RT * 16 + r) * 2 + 1] = total;
+        }
+      } else {
+        const int i = r / a.G, head = h * a.G + (r - i * a.G);
+        const float inv = total == 0.f ? 0.f : 1.f / total;
+        if (d < q.D)
+          *(u32x2*)((uint16_t*)a.out + (int64_t)(a.tok[b] + i) * a.o_token +
+                    (int64_t)head * a.o_head + d) =
+              u32x2{T::pack(v[0] * inv, v[1] * inv), T::pack(v[2] * inv, v[3] * inv)};
+        if (a.lse && d == 0)
+          a.lse[(int64_t)(a.row0 + a.tok[b] + i) * a.q_heads + head] =
+              total == 0.f ? -INFINITY : (top + __log2f(total)) * kLn2;
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Many rows (prompt chunks): a workgroup takes 128 rows (queries and heads of a
+// group together, so that all share the head's tokens), 32 to a wave, and 64
+// tokens at a time: codes are converted once for the four waves and kept in LDS
+// as 16-bit rows, two tiles in turn.  32x32x16 products; values come out of LDS
+// transposed (ds_read_tr).
+// Bound by the matrix units, the exponentials and LDS.
+// ---------------------------------------------------------------------------
+constexpr int kTileTokens = 64;
+
+__device__ __forceinline__ u32x2 read_tr(const uint8_t* p) {
+  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p));
+}
+
+template <bool BF16, int DP>
+__global__ void __launch_bounds__(kThreads) attend_tile_kernel(AttendArgs a, int direct) {
+  using T = Ty<BF16>;
+  constexpr int KS = DP / 16, DB = DP / 32;
+  constexpr int kPitch = DP * 2 + 16, vPitch = DP * 2 + 32;  // bytes of a token's row in LDS
+  constexpr int kUnits = DP / 16;                            // 16 codes each
+  constexpr int UL = kTileTokens * kUnits / kThreads;        // units a thread loads (K, and V)
+  static_assert(UL >= 1, "");
+  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+  constexpr int kBuf = kTileTokens * (kPitch + vPitch);
+  float* const extra = (float*)(lds + 2 * kBuf);  // [2][64] positions, [2][64] mapped, [2][4] flags
+  const QLayout& q = a.q;
+  const int tid = threadIdx.x, wave = tid >> 6, l = tid & 63, c = l & 31, hf = l >> 5;
+
+  const int item = blockIdx.x, b = seq_of(a, item), sb = a.b0 + b;
+  const int len = a.len[b], nq = a.tok[b + 1] - a.tok[b], rows = nq * a.G;
+  const int nsplit = max(1, (len + a.chunk - 1) / a.chunk);
+  const int tiles = (rows + kTileRows - 1) / kTileRows;
+  const int k = item - a.item[b], h = k / (tiles * nsplit), kk = k - h * tiles * nsplit;
+  // the last rows see the most tokens: they go first
+  const int tile = tiles - 1 - kk / nsplit, split = kk % nsplit;
+  const int r0 = tile * kTileRows, r = r0 + wave * 32 + c;
+  const bool on = r < rows;
+  const int i0 = r / a.G, head = h * a.G + (r - i0 * a.G);
+  const int limit = on ? len - nq + i0 : -1;
+  const int all_see = len - nq + r0 / a.G;
+  const int last = len - nq + (min(rows, r0 + kTileRows) - 1) / a.G;  // the last slot seen
+  const int begin = split * a.chunk, end = min(min(begin + a.chunk, len), last + 1);
+
+  const int64_t slab = 2 * (int64_t)a.layer;
+  const uint8_t* kb = q.codes + slab * q.s_slab + sb * q.s_b + h * q.s_h;
+  const uint8_t* vb = kb + q.s_slab;
+  const float* sk = q.scale + slab * q.c_slab + sb * q.c_b + h * q.c_h;
+  const int64_t slots = (((int64_t)a.layer * q.batch + sb) * q.heads + h) * (int64_t)q.cap;
+
+  u32x4 qr[KS];
+  {
+    const uint16_t* src = (const uint16_t*)a.query +
+                          (int64_t)(on ? a.tok[b] + i0 : 0) * a.q_token + (int64_t)head * a.q_head;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const int d = s * 16 + hf * 8;
+      qr[s] = on && d < q.D ? *(const u32x4*)(src + d) : u32x4{0, 0, 0, 0};
+    }
+  }
+  float slope = 0.f, here = 0.f;
+  if (a.slopes && limit >= 0) {
+    slope = a.slopes[head] * kLog2e;
+    here = (float)(q.position ? q.position[slots + limit] : limit);
+  }
+
+  // Loading: unit u = tid + 256 i is 16 codes of token u / kUnits.
+  struct Codes {
+    u32x4 k[UL], v[UL];
+    float ks[UL], vs[UL], at;
+    int hole;
+  };
+  auto block_of = [&](int (&blk)[UL], int t) {
+#pragma unroll
+    for (int i = 0; i < UL; ++i) {
+      const int tok = min(t + (tid + kThreads * i) / kUnits, len - 1), j = q.d_bs.div(tok);
+      blk[i] = q.bt ? q.bt[(int64_t)sb * q.max_blocks + j] : j;
+    }
+  };
+  auto load = [&](Codes& x, const int (&blk)[UL], int t) {
+    x.hole = 0;
+#pragma unroll
+    for (int i = 0; i < UL; ++i) {
+      const int u = tid + kThreads * i;
+      const int tok = min(t + u / kUnits, len - 1), j = q.d_bs.div(tok);
+      const bool hole = q.bt && (uint32_t)blk[i] >= (uint32_t)q.num_blocks;
+      const bool out = u % kUnits * 16 >= q.D;
+      const int64_t bk = hole ? 0 : blk[i];
+      const int64_t o = bk * q.s_blk + (int64_t)(tok - j * q.bs) * q.D + (out ? 0 : u % kUnits * 16);
+      x.k[i] = *(const u32x4*)(kb + o);
+      x.v[i] = *(const u32x4*)(vb + o);
+      x.ks[i] = sk[bk * q.c_blk];
+      x.vs[i] = sk[bk * q.c_blk + q.c_slab];
+      if (hole || out) x.k[i] = x.v[i] = u32x4{0, 0, 0, 0};
+      x.hole |= (int)hole << i;
+    }
+    if (a.slopes && tid < kTileTokens) {
+      const int tok = min(t + tid, len - 1);
+      x.at = (float)(q.position ? q.position[slots + tok] : tok);
+    }
+  };
+  auto store = [&](const Codes& x, int buf, bool mask) {
+    uint8_t* kl = lds + buf * kBuf;
+    uint8_t* vl = kl + kTileTokens * kPitch;
+    uint32_t odd = 0;
+#pragma unroll
+    for (int i = 0; i < UL; ++i) {
+      const int u = tid + kThreads * i, tok = u / kUnits, p = u % kUnits;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        u32x4 y, z;
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          y[2 * w] = T::template cvt<false>(x.k[i][2 * e + w], x.ks[i]);
+          y[2 * w + 1] = T::template cvt<true>(x.k[i][2 * e + w], x.ks[i]);
+          z[2 * w] = T::template cvt<false>(x.v[i][2 * e + w], x.vs[i]);
+          z[2 * w + 1] = T::template cvt<true>(x.v[i][2 * e + w], x.vs[i]);
+        }
+        *(u32x4*)(kl + tok * kPitch + p * 32 + e * 16) = y;
+        *(u32x4*)(vl + tok * vPitch + p * 32 + e * 16) = z;
+      }
+      if (mask)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) odd |= nan_bytes(x.v[i][w]);
+      if (p == 0) extra[128 + buf * 64 + tok] = (x.hole >> i) & 1 ? 0.f : 1.f;
+    }
+    const bool holes = __any(x.hole != 0), nans = __any(odd != 0);
+    if (l == 0) ((int*)extra)[256 + buf * 4 + wave] = (int)holes | (int)nans << 1;
+    if (a.slopes && tid < kTileTokens) extra[buf * 64 + tid] = x.at;
+  };
+
+  f32x16 o[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+  float m = kLow, sum = 0.f;
+
+  Codes x;
+  int blk[UL];
+  if (begin < end) {
+    block_of(blk, begin);
+    load(x, blk, begin);
+    block_of(blk, begin + kTileTokens);
+    store(x, 0, begin + kTileTokens - 1 > all_see);
+  }
+  __syncthreads();
+  int buf = 0;
+  for (int t = begin; t < end; t += kTileTokens, buf ^= 1) {
+    const bool more = t + kTileTokens < end;
+    if (more) {
+      load(x, blk, t + kTileTokens);
+      block_of(blk, t + 2 * kTileTokens);
+    }
+    const uint8_t* kl = lds + buf * kBuf;
+    const uint8_t* vl = kl + kTileTokens * kPitch;
+    const int* fl = (const int*)extra + 256 + buf * 4;
+    const int flags = __builtin_amdgcn_readfirstlane(fl[0] | fl[1] | fl[2] | fl[3]);
+    const bool mask = t + kTileTokens - 1 > all_see || (flags & 1);
+
+    f32x16 s[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[u][i] = 0.f;
+#pragma unroll
+      for (int e = 0; e < KS; ++e) {
+        const u32x4 y = *(const u32x4*)(kl + (u * 32 + c) * kPitch + e * 32 + hf * 16);
+        s[u] = T::mma32(y, qr[e], s[u]);
+      }
+    }
+    settle(s[0]);
+    settle(s[1]);
+    uint32_t seen = 0;  // bit u * 16 + i: token t + 32 u + (i / 4) * 8 + hf * 4 + i % 4
+    float most = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[u][i] *= a.scale2;
+        const int at = u * 32 + (i / 4) * 8 + hf * 4 + i % 4;
+        if (a.slopes) s[u][i] += slope * (extra[buf * 64 + at] - here);
+        if (mask) {
+          const bool sees = t + at <= limit && extra[128 + buf * 64 + at] != 0.f;
+          s[u][i] = sees ? s[u][i] : -INFINITY;
+          seen |= (uint32_t)sees << (u * 16 + i);
+        }
+        most = fmaxf(most, s[u][i]);
+      }
+    }
+    if (__any(most > m + (kSlack + T::kLift))) {
+      float up = fmaxf(most - T::kLift, m);
+      up = fmaxf(up, __shfl_xor(up, 32));
+      const float f = exp2_(m - up);
+      m = up;
+      sum *= f;
+#pragma unroll
+      for (int d = 0; d < DB; ++d) o[d] = o[d] * f;
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {  // 16 tokens: slots hf * 8 + 0..7 of the inner axis
+        u32x4 p;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float p0 = exp2_(s[u][e * 8 + 2 * i] - m), p1 = exp2_(s[u][e * 8 + 2 * i + 1] - m);
+          sum += p0 + p1;
+          p[i] = T::pack(p0, p1);
+        }
+        const uint8_t* row = vl + (u * 32 + e * 16 + hf * 4 + ((l & 15) >> 2)) * vPitch +
+                             ((l >> 4) & 1) * 32 + (l & 3) * 8;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          const u32x2 v0 = read_tr(row + d * 64), v1 = read_tr(row + 8 * vPitch + d * 64);
+          u32x4 v = {v0[0], v0[1], v1[0], v1[1]};
+          if (mask && (flags & 2)) {  // as in the kernel above
+            u32x4 is, sees;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const bool n0 = (v[i] & 0x7fff) > T::kInf, n1 = ((v[i] >> 16) & 0x7fff) > T::kInf;
+              is[i] = (n0 ? T::kOne : 0) | (n1 ? T::kOne << 16 : 0);
+              v[i] &= (n0 ? 0 : 0xffffu) | (n1 ? 0 : 0xffff0000u);
+              const int bit = u * 16 + e * 8 + 2 * i;
+              sees[i] = ((seen >> bit) & 1) * T::kOne | ((seen >> (bit + 1)) & 1) * (T::kOne << 16);
+            }
+            f32x16 z;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[i] = 0.f;
+            z = T::mma32(is, sees, z);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] = z[i] > 0.f ? NAN : o[d][i];
+          }
+          o[d] = T::mma32(v, p, o[d]);
+        }
+      }
+    if (more) store(x, buf ^ 1, t + 2 * kTileTokens - 1 > all_see);
+    __syncthreads();
+  }
+
+  sum += __shfl_xor(sum, 32);
+  if (!on) return;
+  if (!direct) {
+    const int64_t at = (int64_t)item * kTileRows + wave * 32 + c;
+    if (hf == 0) {
+      a.ml[at * 2] = m;
+      a.ml[at * 2 + 1] = sum;
+    }
+    if (begin >= end) return;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4)
+        *(f32x4*)(a.part + at * DP + d * 32 + (i / 4) * 8 + hf * 4) =
+            f32x4{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
+    return;
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  uint16_t* out = (uint16_t*)a.out + (int64_t)(a.tok[b] + i0) * a.o_token + (int64_t)head * a.o_head;
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const int at = d * 32 + (i / 4) * 8 + hf * 4;
+      if (at < q.D)
+        *(u32x2*)(out + at) = u32x2{T::pack(o[d][i] * inv, o[d][i + 1] * inv),
+                                    T::pack(o[d][i + 2] * inv, o[d][i + 3] * inv)};
+    }
+  if (hf == 0) {
+    const float lse2 = m + __log2f(sum);
+    const int64_t row = (int64_t)(a.tok[b] + i0) * a.q_heads + head;
+    if (a.lse) a.lse[(int64_t)a.row0 * a.q_heads + row] = sum == 0.f ? -INFINITY : lse2 * kLn2;
+    if (a.weigh) a.row_lse[row] = sum == 0.f ? INFINITY : lse2;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Joins the splits of the kernels above: R rows a work item.  The workgroup of a
+// split finds every row's sum over the splits, adds up the results of its share
+// of the rows, and, where the scores were kept, the weights of its own tokens.
+// ---------------------------------------------------------------------------
+template <bool BF16, int DP>
+__global__ void __launch_bounds__(kThreads) attend_join_kernel(AttendArgs a, int R) {
+  using T = Ty<BF16>;
+  __shared__ float top[kTileRows], total[kTileRows], acc[kThreads];
+  const QLayout& q = a.q;
+  const int tid = threadIdx.x, wave = tid >> 6, l = tid & 63;
+  const int item = blockIdx.x, b = seq_of(a, item), sb = a.b0 + b;
+  const int len = a.len[b], nq = a.tok[b + 1] - a.tok[b], rows = nq * a.G;
+  const int nsplit = max(1, (len + a.chunk - 1) / a.chunk);
+  const int tiles = (rows + R - 1) / R;
+  const int k = item - a.item[b], h = k / (tiles * nsplit), kk = k - h * tiles * nsplit;
+  const int tile = tiles - 1 - kk / nsplit, split = kk % nsplit;
+  const int r0 = tile * R, nr = min(R, rows - r0);
+  const int64_t first = (int64_t)item - split;
+
+  for (int r = wave; r < nr; r += 4) {
+    float m = kLow;
+    for (int s = l; s < nsplit; s += 64) m = fmaxf(m, a.ml[((first + s) * R + r) * 2]);
+    for (int x = 32; x; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
+    float sum = 0.f;
+    for (int s = l; s < nsplit; s += 64)
+      sum += a.ml[((first + s) * R + r) * 2 + 1] * exp2_(a.ml[((first + s) * R + r) * 2] - m);
+    for (int x = 32; x; x >>= 1) sum += __shfl_xor(sum, x);
+    if (l == 0) {
+      top[r] = m;
+      total[r] = sum;
+    }
+  }
+  __syncthreads();
+  for (int r = split; r < nr; r += nsplit) {
+    constexpr int P = kThreads / DP;  // threads to a dim
+    const int d = tid % DP, i = (r0 + r) / a.G, head = h * a.G + (r0 + r - i * a.G);
+    const float m = top[r], inv = total[r] == 0.f ? 0.f : 1.f / total[r];
+    float v = 0.f;
+    for (int s = tid / DP; s < nsplit; s += P) {
+      const int64_t at = (first + s) * R + r;
+      if (a.ml[at * 2 + 1] != 0.f) v += a.part[at * DP + d] * exp2_(a.ml[at * 2] - m);
+    }
+    if constexpr (P > 1) {
+      __syncthreads();
+      acc[tid] = v;
+      __syncthreads();
+      if (tid < DP)
+        for (int p = 1; p < P; ++p) v += acc[tid + p * DP];
+    }
+    if (tid < q.D) {
+      const uint32_t w = T::pack(v * inv, 0.f);
+      ((uint16_t*)a.out)[(int64_t)(a.tok[b] + i) * a.o_token + (int64_t)head * a.o_head + d] =
+          (uint16_t)w;
+    }
+    if (tid == 0) {
+      const float lse2 = m + __log2f(total[r]);
+      const int64_t row = (int64_t)(a.tok[b] + i) * a.q_heads + head;
+      if (a.lse)
+        a.lse[(int64_t)a.row0 * a.q_heads + row] = total[r] == 0.f ? -INFINITY : lse2 * kLn2;
+      if (a.row_lse) a.row_lse[row] = total[r] == 0.f ? INFINITY : lse2;
+    }
+  }
+  if (!a.weigh || !a.scores) return;
+  for (int r = tid; r < nr; r += kThreads)
+    total[r] = total[r] == 0.f ? INFINITY : top[r] + __log2f(total[r]);
+  __syncthreads();
+  const int64_t pitch = (len + 31) & ~31;
+  const float* sc = a.scores + (int64_t)a.soff[b] * 32 + (int64_t)h * rows * pitch;
+  float* weight = q.weight + (((int64_t)a.layer * q.batch + sb) * q.heads + h) * (int64_t)q.cap;
+  const int c0 = split * a.chunk, cn = min(a.chunk, len - c0);
+  for (int t = tid; t < cn; t += kThreads) {
+    float w = 0.f;
+    for (int r = 0; r < nr; ++r) {
+      const float s2 = sc[r * pitch + c0 + t];  // hidden tokens get 0 also where lse is NaN
+      w += s2 == -INFINITY ? 0.f : exp2_(s2 - total[r]);
+    }
+    weight[c0 + t] = a.decay == 0.f ? w : a.decay * weight[c0 + t] + w;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Weights from many rows: a workgroup takes 128 tokens of a head, 32 to a wave,
+// and every row that may see them; p = exp2(s2 - lse2).  Each sum is one lane's
+// and the lanes' are added in a fixed order.  Bound as the product is.
+// ---------------------------------------------------------------------------
+template <bool BF16, int DP>
+__global__ void __launch_bounds__(kThreads) attend_weigh_kernel(AttendArgs a) {
+  using T = Ty<BF16>;
+  constexpr int KS = DP / 16, kPitch = DP * 2 + 16, UL = 32 * DP * 2 / 16 / kThreads;
+  __shared__ __attribute__((aligned(16))) uint8_t ql[2][32 * kPitch];
+  __shared__ float lse[2][32], slopes[2][32], heres[2][32];
+  const QLayout& q = a.q;
+  const int tid = threadIdx.x, wave = tid >> 6, l = tid & 63, c = l & 31, hf = l >> 5;
+  const int item = blockIdx.x, b = seq_of(a, item), sb = a.b0 + b;
+  const int len = a.len[b], nq = a.tok[b + 1] - a.tok[b], rows = nq * a.G;
+  const int tiles = (len + kWeighTokens - 1) / kWeighTokens;
+  const int k = item - a.item[b], h = k / tiles, t0 = (k - h * tiles) * kWeighTokens;
+  const int tw = t0 + wave * 32;  // this wave's tokens
+
+  const int64_t slab = 2 * (int64_t)a.layer;
+  const int64_t slots = (((int64_t)a.layer * q.batch + sb) * q.heads + h) * (int64_t)q.cap;
+  u32x4 kr[KS];
+  uint32_t mapped;  // bit i: token tw + i
+  {
+    const int tok = min(tw + c, len - 1), j = q.d_bs.div(tok);
+    int64_t blk = q.bt ? q.bt[(int64_t)sb * q.max_blocks + j] : j;
+    const bool hole = q.bt && (uint64_t)blk >= (uint64_t)q.num_blocks;
+    blk = hole ? 0 : blk;
+    mapped = (uint32_t)__ballot(!hole);
+    const uint8_t* p = q.codes + slab * q.s_slab + sb * q.s_b + h * q.s_h + blk * q.s_blk +
+                       (int64_t)(tok - j * q.bs) * q.D;
+    const float scale = q.scale[slab * q.c_slab + sb * q.c_b + h * q.c_h + blk * q.c_blk];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const int d = s * 16 + hf * 8;
+      u32x2 w = {0, 0};
+      if (d < q.D) w = *(const u32x2*)(p + d);
+      kr[s] = u32x4{T::template cvt<false>(w[0], scale), T::template cvt<true>(w[0], scale),
+                    T::template cvt<false>(w[1], scale), T::template cvt<true>(w[1], scale)};
+    }
+  }
+  float at[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int tok = min(tw + (i / 4) * 8 + hf * 4 + i % 4, len - 1);
+    at[i] = a.slopes ? (float)(q.position ? q.position[slots + tok] : tok) : 0.f;
+  }
+
+  const int before = len - nq;  // query i sees slots up to before + i
+  u32x4 x[UL];
+  float x_lse = 0.f, x_slope = 0.f, x_here = 0.f;
+  auto load = [&](int r0) {
+#pragma unroll
+    for (int i = 0; i < UL; ++i) {
+      const int u = tid + kThreads * i, r = r0 + u / (DP / 8), d = u % (DP / 8) * 8;
+      const int qi = r / a.G, head = h * a.G + (r - qi * a.G);
+      x[i] = u32x4{0, 0, 0, 0};
+      if (r < rows && d < q.D)
+        x[i] = *(const u32x4*)((const uint16_t*)a.query + (int64_t)(a.tok[b] + qi) * a.q_token +
+                               (int64_t)head * a.q_head + d);
+    }
+    if (tid < 32) {
+      const int r = r0 + tid, qi = r / a.G, head = h * a.G + (r - qi * a.G);
+      x_lse = INFINITY;
+      x_slope = x_here = 0.f;
+      if (r < rows) {
+        x_lse = a.row_lse[(int64_t)(a.tok[b] + qi) * a.q_heads + head];
+        if (a.slopes && before + qi >= 0) {
+          x_slope = a.slopes[head] * kLog2e;
+          x_here = (float)(q.position ? q.position[slots + before + qi] : before + qi);
+        }
+      }
+    }
+  };
+  auto store = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < UL; ++i) {
+      const int u = tid + kThreads * i;
+      *(u32x4*)(ql[buf] + u / (DP / 8) * kPitch + u % (DP / 8) * 16) = x[i];
+    }
+    if (tid < 32) {
+      lse[buf][tid] = x_lse;
+      slopes[buf][tid] = x_slope;
+      heres[buf][tid] = x_here;
+    }
+  };
+
+  float sum[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) sum[i] = 0.f;
+  // the first row that sees the workgroup's first token
+  const int from = max(0, t0 - before) * a.G & ~31;
+  int buf = 0;
+  if (from < rows) {
+    load(from);
+    store(0);
+  }
+  __syncthreads();
+  for (int r0 = from; r0 < rows; r0 += 32, buf ^= 1) {
+    const bool more = r0 + 32 < rows;
+    if (more) load(r0 + 32);
+    f32x16 s;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+    for (int e = 0; e < KS; ++e)
+      s = T::mma32(kr[e], *(const u32x4*)(ql[buf] + c * kPitch + e * 32 + hf * 16), s);
+    settle(s);
+    const float lse2 = lse[buf][c], sl = slopes[buf][c], here = heres[buf][c];
+    const int limit = before + (r0 + c) / a.G;
+    const bool mask = before + r0 / a.G < tw + 31 || mapped != 0xffffffffu;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int o = (i / 4) * 8 + hf * 4 + i % 4;
+      float y = s[i] * a.scale2;
+      if (a.slopes) y += sl * (at[i] - here);
+      float p = exp2_(y - lse2);
+      if (mask) p = tw + o <= limit && ((mapped >> o) & 1) && lse2 != INFINITY ? p : 0.f;
+      sum[i] += p;
+    }
+    if (more) store(buf ^ 1);
+    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+#pragma unroll
+    for (int x = 16; x; x >>= 1) sum[i] += __shfl_xor(sum[i], x);
+    const int tok = tw + (i / 4) * 8 + hf * 4 + i % 4;
+    if (c == i && tok < len) {
+      float* w = q.weight + slots + tok;
+      *w = a.decay == 0.f ? sum[i] : a.decay * *w + sum[i];
+    }
+  }
+}
+
+int padded(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
+
+template <typename... More>
+hipError_t launch(const void* fn, uint32_t groups, size_t lds, hipStream_t s, const AttendArgs& a,
+                  More... more) {
+  void* args[] = {const_cast<AttendArgs*>(&a), &more...};
+  return hipLaunchKernel(fn, dim3(groups), dim3(kThreads), args, lds, s);
+}
+
+template <bool BF16, int DP>
+struct Kernels {
+  static const void* split(int rt) {
+    if (rt == 1) return (const void*)&attend_split_kernel<BF16, DP, 1>;
+    if (rt == 2) return (const void*)&attend_split_kernel<BF16, DP, 2>;
+    if constexpr (DP < 256) return (const void*)&attend_split_kernel<BF16, DP, 4>;
+    return nullptr;
+  }
+  static const void* tile() { return (const void*)&attend_tile_kernel<BF16, DP>; }
+  static const void* join() { return (const void*)&attend_join_kernel<BF16, DP>; }
+  static const void* weigh() { return (const void*)&attend_weigh_kernel<BF16, DP>; }
+};
+
+// f(Kernels<type, padded head_dim>) for a launch's type and head_dim
+template <typename F>
+const void* pick(const AttendArgs& a, F f) {
+  const int dp = padded(a.q.D);
+  if (a.bf16)
+    return dp == 64    ? f(Kernels<true, 64>())
+           : dp == 128 ? f(Kernels<true, 128>())
+                       : f(Kernels<true, 256>());
+  return dp == 64    ? f(Kernels<false, 64>())
+         : dp == 128 ? f(Kernels<false, 128>())
+                     : f(Kernels<false, 256>());
+}
+
+}  // namespace
+
+hipError_t launch_attend_split(const AttendArgs& a, int rt, bool direct, hipStream_t s) {
+  const void* fn = pick(a, [&](auto k) { return decltype(k)::split(rt); });
+  const size_t tables = (size_t)a.chunk * (a.slopes ? 16 : 12);
+  const size_t join = (size_t)4 * 16 * padded(a.q.D) * 4 + (size_t)4 * rt * 16 * 8;
+  return launch(fn, (uint32_t)a.items, tables > join ? tables : join, s, a, (int)direct);
+}
+
+hipError_t launch_attend_tile(const AttendArgs& a, bool direct, hipStream_t s) {
+  const void* fn = pick(a, [](auto k) { return decltype(k)::tile(); });
+  const size_t lds = (size_t)2 * kTileTokens * (padded(a.q.D) * 4 + 48) + 264 * 4;
+  return launch(fn, (uint32_t)a.items, lds, s, a, (int)direct);
+}
+
+hipError_t launch_attend_join(const AttendArgs& a, int rows, hipStream_t s) {
+  return launch(pick(a, [](auto k) { return decltype(k)::join(); }), (uint32_t)a.items, 0, s, a,
+                rows);
+}
+
+hipError_t launch_attend_weigh(const AttendArgs& a, hipStream_t s) {
+  return launch(pick(a, [](auto k) { return decltype(k)::weigh(); }), (uint32_t)a.items, 0, s, a);
+}
+
+}  // namespace dv

@@ -1,0 +1,120 @@
+// Launch descriptors shared by the host side (dv_attn.cpp) and the kernels
+// (dv_quant.hip, dv_attend.hip, dv_evict.hip) of the 8-bit cache operators.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "dv_internal.h"
+
+namespace dv {
+
+// Sequences of one launch: their tables travel in the kernel arguments (four
+// int32 each, 3 KB in all).
+constexpr int kQSeqs = 192;
+
+// Where an 8-bit cache's codes (bytes) and scales (floats) lie.  Token t of
+// (sequence b, head h) in slab = 2 * layer + half: block j = t / bs, blk = table
+// entry j of b (paged) or j itself (dense);
+//   code  slab * s_slab + b * s_b + blk * s_blk + h * s_h + (t % bs) * D
+//   scale slab * c_slab + b * c_b + blk * c_blk + h * c_h
+struct QLayout {
+  uint8_t* codes;
+  float* scale;
+  const int32_t* bt;  // paged: [batch][max_blocks], else null
+  float* weight;      // [layer][batch][head][cap] or null
+  int32_t* position;
+  int64_t s_slab, s_b, s_blk, s_h;
+  int64_t c_slab, c_b, c_blk, c_h;
+  int32_t bs, D, heads, batch;
+  int32_t num_blocks, max_blocks;
+  int32_t cap, pad;
+  FastDiv d_bs;
+};
+
+// The smallest power of two, at least 2^-64, whose 448-fold is at least amax
+// (448 = 1.75 * 2^8): from amax's exponent, one more where its fraction exceeds
+// 1.75.
+__device__ __forceinline__ float scale_for(float amax) {
+  const uint32_t b = __float_as_uint(amax);
+  const int e = (int)(b >> 23) + ((b & 0x7fffff) > 0x600000) - 8;
+  return __uint_as_float((uint32_t)max(e, 127 - 64) << 23);
+}
+
+// 1 / p for a power of two of [2^-64, 2^120].
+__device__ __forceinline__ float inverse(float p) {
+  return __uint_as_float((254u << 23) - __float_as_uint(p));
+}
+
+// ---- dv_quant_in ----
+// A work item is one block of one head of one sequence; item[] counts those of
+// earlier sequences.  A group of 1 << lanes_log2 lanes takes an item.
+struct QuantArgs {
+  QLayout q;
+  const uint8_t* wire;  // advanced to this launch's first sequence
+  int64_t w_slab;       // wire bytes per slab (layer, half)
+  int32_t slab0, b0, nseq, items;
+  int32_t lanes_log2, bf16;
+  int32_t item[kQSeqs];     // INT32_MAX past the last
+  int32_t tok[kQSeqs + 1];  // tokens of earlier sequences
+  int32_t t0[kQSeqs];
+};
+static_assert(sizeof(QuantArgs) <= 3584, "arguments stay under 4 KB");
+hipError_t launch_quant(const QuantArgs& a, uint32_t nslabs, hipStream_t s);
+
+// ---- dv_attend ----
+// Queries of a sequence and the heads of a group are rows r = i * G + g.
+struct AttendArgs {
+  QLayout q;
+  const void* query;
+  void* out;
+  int64_t q_token, q_head, o_token, o_head;  // elements
+  const float* slopes;
+  float* lse;
+  float* part;    // split rows: [item][RT * 16 rows][Dp] sums, then [item][rows][2] max, sum
+  float* ml;
+  float* scores;  // weigh, split rows: [sequence][head][row][padded tokens], log2 units
+  float* row_lse; // weigh, many rows: [row of the call][q_heads], log2 units
+  float scale2;   // scale * log2 e
+  float decay;
+  int32_t layer, b0, nseq, items;
+  int32_t G, q_heads, chunk;  // chunk: tokens of a split (rows of a tile where there are many)
+  int32_t weigh, bf16, row0;  // row0: rows of q before this launch's
+  int32_t item[kQSeqs];       // work items of earlier sequences; INT32_MAX past the last
+  int32_t tok[kQSeqs + 1];    // queries of earlier sequences
+  int32_t len[kQSeqs];        // tokens in the cache
+  int32_t soff[kQSeqs];       // scores of earlier sequences, in 32 floats
+};
+static_assert(sizeof(AttendArgs) <= 3800, "arguments stay under 4 KB");
+// Few rows: RT tiles of 16 rows (1, 2, 4), the token axis split into chunks of
+// a.chunk tokens; `direct`: one chunk a sequence, results go straight to out.
+hipError_t launch_attend_split(const AttendArgs& a, int rt, bool direct, hipStream_t s);
+hipError_t launch_attend_join(const AttendArgs& a, int rows, hipStream_t s);
+// Many rows: tiles of kTileRows rows.
+constexpr int kTileRows = 128;
+hipError_t launch_attend_tile(const AttendArgs& a, bool direct, hipStream_t s);
+// Column sums of the probabilities, from the rows' lse.
+constexpr int kWeighTokens = 128;
+hipError_t launch_attend_weigh(const AttendArgs& a, hipStream_t s);
+
+// Tokens of a wave's step over the cache, and of a workgroup's (four waves).
+constexpr int kSplitStep = 32;
+constexpr int kSplitRound = 4 * kSplitStep;
+constexpr int kSplitChunkMax = 2048;
+
+// ---- dv_evict ----
+struct EvictArgs {
+  QLayout s, d;
+  int32_t* kept;
+  int32_t kept_stride, recent, l0, nl;
+  int32_t b0, nseq, in_place, most;  // most: tokens of the longest sequence
+  int32_t blocks, pad;  // most result blocks of a sequence
+  FastDiv d_du;          // by 16-code units of a token
+  int32_t len[kQSeqs];
+  int32_t keep[kQSeqs];
+};
+static_assert(sizeof(EvictArgs) <= 3584, "arguments stay under 4 KB");
+hipError_t launch_evict_select(const EvictArgs& a, hipStream_t s);
+hipError_t launch_evict_move(const EvictArgs& a, hipStream_t s);
+
+}  // namespace dv
