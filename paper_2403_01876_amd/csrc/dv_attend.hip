@@ -16,6 +16,8 @@
 // at most, which costs no precision.  kLift is 7 for f16, whose probabilities stay
 // normal numbers down to 2^-21 of the largest so (a value 2^12 times another's
 // shows their rounding below 2^-14 otherwise), and 0 for bf16.
+#include <type_traits>
+
 #include "dv_attn_internal.h"
 
 namespace dv {
@@ -92,12 +94,32 @@ struct Ty<true> {
 };
 
 // The sequence that holds work item `item` (as find_seq of the streaming
-// kernels: the count of first items at or below it names it).
-__device__ __forceinline__ int seq_of(const AttendArgs& a, int item) {
+// kernels: the count of first items at or below it names it).  Lanes load their
+// sequences' entries together, so that the common launch of up to 64 sequences
+// waits for memory once.
+struct Seq {
+  int b, k;           // index in the launch; the item's index in the sequence
+  int len, tok, nq;   // tokens in the cache; queries of earlier sequences; its own
+};
+__device__ __forceinline__ Seq seq_of(const AttendArgs& a, int item) {
   const int lane = threadIdx.x & 63;
-  int below = 0;
-  for (int i = 0; i < a.nseq; i += 64) below += __popcll(__ballot(a.item[i + lane] <= item));
-  return __builtin_amdgcn_readfirstlane(below - 1);
+  const int first = a.item[lane], len = a.len[lane], t0 = a.tok[lane], t1 = a.tok[lane + 1];
+  Seq q;
+  q.b = __popcll(__ballot(first <= item)) - 1;
+  if (q.b == 63 && a.nseq > 64) {
+    for (int i = 64; i < a.nseq; i += 64) q.b += __popcll(__ballot(a.item[i + lane] <= item));
+    q.b = __builtin_amdgcn_readfirstlane(q.b);
+    q.k = item - a.item[q.b];
+    q.len = a.len[q.b];
+    q.tok = a.tok[q.b];
+    q.nq = a.tok[q.b + 1] - q.tok;
+    return q;
+  }
+  q.k = item - __builtin_amdgcn_readlane(first, q.b);
+  q.len = __builtin_amdgcn_readlane(len, q.b);
+  q.tok = __builtin_amdgcn_readlane(t0, q.b);
+  q.nq = __builtin_amdgcn_readlane(t1, q.b) - q.tok;
+  return q;
 }
 
 // Called on products' results before any branch: ends the wait for them in the
@@ -108,6 +130,14 @@ __device__ __forceinline__ int seq_of(const AttendArgs& a, int item) {
 template <typename V>
 __device__ __forceinline__ void settle(V& a) {
   asm volatile("s_nop 12" : "+v"(a));
+}
+
+// A barrier after which the workgroup's LDS writes are seen; unlike
+// __syncthreads it leaves loads from memory in flight.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
 // 0x80 in each byte of w that is a NaN code.
@@ -134,23 +164,29 @@ __device__ __forceinline__ uint32_t highs(uint32_t a, uint32_t b) {
 // Bound by HBM.
 // ---------------------------------------------------------------------------
 template <bool BF16, int DP, int RT>
-__global__ void __launch_bounds__(kThreads) attend_split_kernel(AttendArgs a, int direct) {
+__global__ void __launch_bounds__(kThreads, split_groups(DP, RT))
+    attend_split_kernel(AttendArgs a, int direct) {
   using T = Ty<BF16>;
   constexpr int KL = DP / 64, VW = DP / 64, KS = DP / 32, OJ = DP / 16;
+  constexpr bool kInLds = RT > 1;  // the queries
+  __shared__ int odd[4];
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   const QLayout& q = a.q;
   const int tid = threadIdx.x, wave = tid >> 6, l = tid & 63, c = l & 15, g = l >> 4;
 
-  const int item = blockIdx.x, b = seq_of(a, item), sb = a.b0 + b;
-  const int len = a.len[b], nq = a.tok[b + 1] - a.tok[b], rows = nq * a.G;
+  const int item = blockIdx.x;
+  const Seq seq = seq_of(a, item);
+  const int b = seq.b, sb = a.b0 + b, len = seq.len, nq = seq.nq, rows = nq * a.G;
   const int nsplit = max(1, (len + a.chunk - 1) / a.chunk);
-  const int k = item - a.item[b], h = k / nsplit, c0 = (k - h * nsplit) * a.chunk;
+  const int h = seq.k / nsplit, c0 = (seq.k - h * nsplit) * a.chunk;
   const int cn = min(a.chunk, len - c0);  // tokens of this chunk
 
-  uint32_t* off = (uint32_t*)lds;         // each token's row, in 16 bytes from the head's base
-  float* ks = (float*)lds + a.chunk;      // scales; 0: an unmapped block
-  float* vs = (float*)lds + 2 * a.chunk;
-  float* pos = (float*)lds + 3 * a.chunk;
+  u32x4* const ql = (u32x4*)lds;  // [RT][KS][lane]
+  float* const tables = (float*)(lds + (kInLds ? RT * KS * 1024 : 0));
+  uint32_t* off = (uint32_t*)tables;  // each token's row, in 16 bytes from the head's base
+  float* ks = tables + a.chunk;       // scales; 0: an unmapped block
+  float* vs = tables + 2 * a.chunk;
+  float* pos = tables + 3 * a.chunk;
   const int64_t slab = 2 * (int64_t)a.layer;
   const uint8_t* kb = q.codes + slab * q.s_slab + sb * q.s_b + h * q.s_h;
   const uint8_t* vb = kb + q.s_slab;
@@ -167,26 +203,31 @@ __global__ void __launch_bounds__(kThreads) attend_split_kernel(AttendArgs a, in
       blk = hole ? 0 : blk;
     }
     off[i] = (uint32_t)((blk * q.s_blk + (int64_t)(t - j * q.bs) * q.D) >> 4);
-    ks[i] = hole ? 0.f : sk[blk * q.c_blk];
-    vs[i] = sk[blk * q.c_blk + q.c_slab];
+    ((int*)ks)[i] = hole ? -1 : (int)blk;
     if (a.slopes) pos[i] = (float)(q.position ? q.position[slots + t] : t);
     bad |= hole;
   }
 
   // The queries, and what each column (row c of tile rt) may see.
-  u32x4 qr[RT][KS];
+  u32x4 qr[kInLds ? 1 : KS];
   int limit[RT];
   float slope[RT], here[RT];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const int r = rt * 16 + c, i = r / a.G, head = h * a.G + (r - i * a.G);
     const bool on = r < rows;
-    const uint16_t* src = (const uint16_t*)a.query +
-                          (int64_t)(on ? a.tok[b] + i : 0) * a.q_token + (int64_t)head * a.q_head;
+    if (!kInLds || (rt & 3) == wave || RT < 4) {
+      const uint16_t* src = (const uint16_t*)a.query +
+                            (int64_t)(on ? seq.tok + i : 0) * a.q_token + (int64_t)head * a.q_head;
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      const int d = (s >> 1) * 64 + g * 16 + (s & 1) * 8;
-      qr[rt][s] = on && d < q.D ? *(const u32x4*)(src + d) : u32x4{0, 0, 0, 0};
+      for (int s = 0; s < KS; ++s) {
+        const int d = (s >> 1) * 64 + g * 16 + (s & 1) * 8;
+        const u32x4 x = on && d < q.D ? *(const u32x4*)(src + d) : u32x4{0, 0, 0, 0};
+        if constexpr (kInLds)
+          ql[(rt * KS + s) * 64 + l] = x;
+        else
+          qr[s] = x;
+      }
     }
     limit[rt] = on ? len - nq + i : -1;
     slope[rt] = here[rt] = 0.f;
@@ -195,39 +236,46 @@ __global__ void __launch_bounds__(kThreads) attend_split_kernel(AttendArgs a, in
       here[rt] = (float)(q.position ? q.position[slots + limit[rt]] : limit[rt]);
     }
   }
-  const bool holes = __syncthreads_or(bad);
+  // (LDS is all that the workgroup shares so far: loads may stay in flight)
+  const bool any_bad = __any(bad);
+  if (l == 0) odd[wave] = any_bad;
+  lds_barrier();
+  const bool holes = odd[0] | odd[1] | odd[2] | odd[3];
   const int all_see = len - nq;  // slots up to this one are seen by every row
 
   const int kd = g * 16, vd = c * (DP / 16);
   const bool pad = q.D < DP;
-  struct Tile {
-    u32x4 k[2][KL];
-    uint32_t v[8][VW];
-  };
-  auto load = [&](Tile& x, int t) {
+  // One set of registers holds the step's codes: the next step's keys are asked
+  // for as soon as the products have read these, its values likewise, so loads
+  // are in flight all the time at no cost in registers.
+  u32x4 kx[2][KL];
+  uint32_t vx[8][VW];
+  auto load_k = [&](int t) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const uint8_t* p = kb + (uint64_t)off[t + u * 16 + c] * 16;
 #pragma unroll
       for (int i = 0; i < KL; ++i)
-        x.k[u][i] = *(const u32x4*)(p + (pad && kd + 64 * i >= q.D ? 0 : kd + 64 * i));
+        kx[u][i] = *(const u32x4*)(p + (pad && kd + 64 * i >= q.D ? 0 : kd + 64 * i));
     }
+  };
+  auto load_v = [&](int t) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const u32x4 o = *(const u32x4*)(off + t + u * 16 + g * 4);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const uint8_t* p = vb + (uint64_t)o[i] * 16 + (pad && vd >= q.D ? 0 : vd);
-        if constexpr (VW == 1) x.v[u * 4 + i][0] = *(const uint32_t*)p;
+        if constexpr (VW == 1) vx[u * 4 + i][0] = *(const uint32_t*)p;
         if constexpr (VW == 2) {
           const u32x2 w = *(const u32x2*)p;
-          x.v[u * 4 + i][0] = w[0];
-          x.v[u * 4 + i][1] = w[1];
+          vx[u * 4 + i][0] = w[0];
+          vx[u * 4 + i][1] = w[1];
         }
         if constexpr (VW == 4) {
           const u32x4 w = *(const u32x4*)p;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x.v[u * 4 + i][e] = w[e];
+          for (int e = 0; e < 4; ++e) vx[u * 4 + i][e] = w[e];
         }
       }
     }
@@ -243,31 +291,32 @@ __global__ void __launch_bounds__(kThreads) attend_split_kernel(AttendArgs a, in
     for (int j = 0; j < OJ; ++j) o[rt][j] = f32x4{0, 0, 0, 0};
   }
   const int64_t pitch = (len + 31) & ~31;
-  float* sc = a.scores + (int64_t)a.soff[b] * 32 + (int64_t)h * rows * pitch;
 
-  auto compute = [&](Tile& x, int t) {
+  auto step = [&](int t, auto more) {
     f32x4 s[RT][2];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const float scale = ks[t + u * 16 + c];
+    for (int rt = 0; rt < RT; ++rt) s[rt][0] = s[rt][1] = f32x4{0, 0, 0, 0};
+    const float scale[2] = {ks[t + c], ks[t + 16 + c]};
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) s[rt][u] = f32x4{0, 0, 0, 0};
+    for (int i = 0; i < KL; ++i)
 #pragma unroll
-      for (int i = 0; i < KL; ++i) {
-        u32x4 w = x.k[u][i];
-        if (pad && kd + 64 * i >= q.D) w = u32x4{0, 0, 0, 0};
+      for (int e = 0; e < 2; ++e) {
+        u32x4 y[2];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const u32x4 y = {T::template cvt<false>(w[2 * e], scale),
-                           T::template cvt<true>(w[2 * e], scale),
-                           T::template cvt<false>(w[2 * e + 1], scale),
-                           T::template cvt<true>(w[2 * e + 1], scale)};
+        for (int u = 0; u < 2; ++u) {
+          u32x2 w = {kx[u][i][2 * e], kx[u][i][2 * e + 1]};
+          if (pad && kd + 64 * i >= q.D) w = u32x2{0, 0};
+          y[u] = u32x4{T::template cvt<false>(w[0], scale[u]), T::template cvt<true>(w[0], scale[u]),
+                       T::template cvt<false>(w[1], scale[u]), T::template cvt<true>(w[1], scale[u])};
+        }
 #pragma unroll
-          for (int rt = 0; rt < RT; ++rt)
-            s[rt][u] = T::mma16(y, qr[rt][2 * i + e], s[rt][u]);
+        for (int rt = 0; rt < RT; ++rt) {
+          const u32x4 x = kInLds ? ql[(rt * KS + 2 * i + e) * 64 + l] : qr[kInLds ? 0 : 2 * i + e];
+          s[rt][0] = T::mma16(y[0], x, s[rt][0]);
+          s[rt][1] = T::mma16(y[1], x, s[rt][1]);
         }
       }
-    }
+    if constexpr (decltype(more)::value) load_k(t + kSplitRound);
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       settle(s[rt][0]);
@@ -302,7 +351,8 @@ __global__ void __launch_bounds__(kThreads) attend_split_kernel(AttendArgs a, in
         }
       }
       if (a.weigh && rt * 16 + c < rows) {
-        float* to = sc + (int64_t)(rt * 16 + c) * pitch + first;
+        float* to = a.scores + (int64_t)a.soff[b] * 32 +
+                    ((int64_t)h * rows + rt * 16 + c) * pitch + first;
         *(f32x4*)to = s[rt][0];
         *(f32x4*)(to + 16) = s[rt][1];
       }
@@ -342,17 +392,17 @@ __global__ void __launch_bounds__(kThreads) attend_split_kernel(AttendArgs a, in
 #pragma unroll
       for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int w = 0; w < VW; ++w) any |= nan_bytes(x.v[i][w]);
+        for (int w = 0; w < VW; ++w) any |= nan_bytes(vx[i][w]);
       if (__any(any != 0)) {
 #pragma unroll
         for (int w = 0; w < VW; ++w) {
           uint32_t is[8][2];
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            const uint32_t n = nan_bytes(x.v[i][w]) >> 7;
+            const uint32_t n = nan_bytes(vx[i][w]) >> 7;
             is[i][0] = (n & 1) * T::kOne | ((n >> 8) & 1) * (T::kOne << 16);
             is[i][1] = ((n >> 16) & 1) * T::kOne | ((n >> 24) & 1) * (T::kOne << 16);
-            x.v[i][w] &= ~(n * 0xffu);
+            vx[i][w] &= ~(n * 0xffu);
           }
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt) {
@@ -377,47 +427,50 @@ __global__ void __launch_bounds__(kThreads) attend_split_kernel(AttendArgs a, in
         }
       }
     }
-    float scale[8];
+    const f32x4 v0 = *(const f32x4*)(vs + t + g * 4), v1 = *(const f32x4*)(vs + t + 16 + g * 4);
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const f32x4 w = *(const f32x4*)(vs + t + u * 16 + g * 4);
+    for (int w = 0; w < VW; ++w)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) scale[u * 4 + r] = w[r];
-    }
+      for (int half = 0; half < 2; ++half) {  // dims 0, 1 and 2, 3 of the word
+        uint32_t y[8];
 #pragma unroll
-    for (int w = 0; w < VW; ++w) {
-      uint32_t y[8][2];  // dims 0, 1 and 2, 3 of the word, for each token
+        for (int i = 0; i < 8; ++i) {
+          const float scale = i < 4 ? v0[i] : v1[i & 3];
+          y[i] = half ? T::template cvt<true>(vx[i][w], scale)
+                      : T::template cvt<false>(vx[i][w], scale);
+        }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        y[i][0] = T::template cvt<false>(x.v[i][w], scale[i]);
-        y[i][1] = T::template cvt<true>(x.v[i][w], scale[i]);
-      }
+        for (int e = 0; e < 2; ++e) {
+          u32x4 v;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        u32x4 v;
+          for (int i = 0; i < 4; ++i)
+            v[i] = e ? highs(y[2 * i], y[2 * i + 1]) : lows(y[2 * i], y[2 * i + 1]);
+          const int j = 4 * w + 2 * half + e;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          v[i] = e & 1 ? highs(y[2 * i][e >> 1], y[2 * i + 1][e >> 1])
-                       : lows(y[2 * i][e >> 1], y[2 * i + 1][e >> 1]);
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-          o[rt][4 * w + e] = T::mma16(v, hi[rt], o[rt][4 * w + e]);
-          o[rt][4 * w + e] = T::mma16(v, lo[rt], o[rt][4 * w + e]);
+          for (int rt = 0; rt < RT; ++rt) {
+            o[rt][j] = T::mma16(v, hi[rt], o[rt][j]);
+            o[rt][j] = T::mma16(v, lo[rt], o[rt][j]);
+          }
         }
       }
-    }
+    if constexpr (decltype(more)::value) load_v(t + kSplitRound);
   };
 
-  Tile x, y;
   int t = wave * kSplitStep;
-  if (t < cn) load(x, t);
-  for (; t < cn; t += 2 * kSplitRound) {
-    if (t + kSplitRound < cn) load(y, t + kSplitRound);
-    compute(x, t);
-    if (t + kSplitRound < cn) {
-      if (t + 2 * kSplitRound < cn) load(x, t + 2 * kSplitRound);
-      compute(y, t + kSplitRound);
-    }
+  if (t < cn) {
+    load_k(t);
+    load_v(t);
+  }
+  // The scales follow the first codes: both are on their way at once.
+  for (int i = tid; i < ((cn + kSplitStep - 1) & -kSplitStep); i += kThreads) {
+    const int blk = ((const int*)ks)[i];
+    ks[i] = blk < 0 ? 0.f : sk[blk * q.c_blk];
+    vs[i] = sk[max(blk, 0) * q.c_blk + q.c_slab];
+  }
+  lds_barrier();
+  if (t < cn) {
+    for (; t + kSplitRound < cn; t += kSplitRound) step(t, std::true_type{});
+    step(t, std::false_type{});
   }
 
   // Join the four waves.
@@ -467,11 +520,11 @@ __global__ void __launch_bounds__(kThreads) attend_split_kernel(AttendArgs a, in
         const int i = r / a.G, head = h * a.G + (r - i * a.G);
         const float inv = total == 0.f ? 0.f : 1.f / total;
         if (d < q.D)
-          *(u32x2*)((uint16_t*)a.out + (int64_t)(a.tok[b] + i) * a.o_token +
+          *(u32x2*)((uint16_t*)a.out + (int64_t)(seq.tok + i) * a.o_token +
                     (int64_t)head * a.o_head + d) =
               u32x2{T::pack(v[0] * inv, v[1] * inv), T::pack(v[2] * inv, v[3] * inv)};
         if (a.lse && d == 0)
-          a.lse[(int64_t)(a.row0 + a.tok[b] + i) * a.q_heads + head] =
+          a.lse[(int64_t)(a.row0 + seq.tok + i) * a.q_heads + head] =
               total == 0.f ? -INFINITY : (top + __log2f(total)) * kLn2;
       }
     }
@@ -507,11 +560,12 @@ __global__ void __launch_bounds__(kThreads) attend_tile_kernel(AttendArgs a, int
   const QLayout& q = a.q;
   const int tid = threadIdx.x, wave = tid >> 6, l = tid & 63, c = l & 31, hf = l >> 5;
 
-  const int item = blockIdx.x, b = seq_of(a, item), sb = a.b0 + b;
-  const int len = a.len[b], nq = a.tok[b + 1] - a.tok[b], rows = nq * a.G;
+  const int item = blockIdx.x;
+  const Seq seq = seq_of(a, item);
+  const int b = seq.b, sb = a.b0 + b, len = seq.len, nq = seq.nq, rows = nq * a.G;
   const int nsplit = max(1, (len + a.chunk - 1) / a.chunk);
   const int tiles = (rows + kTileRows - 1) / kTileRows;
-  const int k = item - a.item[b], h = k / (tiles * nsplit), kk = k - h * tiles * nsplit;
+  const int k = seq.k, h = k / (tiles * nsplit), kk = k - h * tiles * nsplit;
   // the last rows see the most tokens: they go first
   const int tile = tiles - 1 - kk / nsplit, split = kk % nsplit;
   const int r0 = tile * kTileRows, r = r0 + wave * 32 + c;
@@ -531,7 +585,7 @@ __global__ void __launch_bounds__(kThreads) attend_tile_kernel(AttendArgs a, int
   u32x4 qr[KS];
   {
     const uint16_t* src = (const uint16_t*)a.query +
-                          (int64_t)(on ? a.tok[b] + i0 : 0) * a.q_token + (int64_t)head * a.q_head;
+                          (int64_t)(on ? seq.tok + i0 : 0) * a.q_token + (int64_t)head * a.q_head;
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       const int d = s * 16 + hf * 8;
@@ -736,7 +790,7 @@ __global__ void __launch_bounds__(kThreads) attend_tile_kernel(AttendArgs a, int
     return;
   }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  uint16_t* out = (uint16_t*)a.out + (int64_t)(a.tok[b] + i0) * a.o_token + (int64_t)head * a.o_head;
+  uint16_t* out = (uint16_t*)a.out + (int64_t)(seq.tok + i0) * a.o_token + (int64_t)head * a.o_head;
 #pragma unroll
   for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -748,90 +802,131 @@ __global__ void __launch_bounds__(kThreads) attend_tile_kernel(AttendArgs a, int
     }
   if (hf == 0) {
     const float lse2 = m + __log2f(sum);
-    const int64_t row = (int64_t)(a.tok[b] + i0) * a.q_heads + head;
+    const int64_t row = (int64_t)(seq.tok + i0) * a.q_heads + head;
     if (a.lse) a.lse[(int64_t)a.row0 * a.q_heads + row] = sum == 0.f ? -INFINITY : lse2 * kLn2;
     if (a.weigh) a.row_lse[row] = sum == 0.f ? INFINITY : lse2;
   }
 }
 
 // ---------------------------------------------------------------------------
-// Joins the splits of the kernels above: R rows a work item.  The workgroup of a
-// split finds every row's sum over the splits, adds up the results of its share
-// of the rows, and, where the scores were kept, the weights of its own tokens.
+// Joins the splits of the kernels above: R rows a work item, a workgroup for each
+// split of a head.  Grid row 0 adds up the results: four dims to a lane, a group
+// of lanes to a row; up to 16 splits are one group's, more are dealt to all of a
+// workgroup's groups.  Grid row 1, where the scores were kept, adds up the
+// weights of the split's own tokens, four to a lane, for which it needs every
+// row's sum.  Bound by latency: two rounds through memory.
 // ---------------------------------------------------------------------------
 template <bool BF16, int DP>
 __global__ void __launch_bounds__(kThreads) attend_join_kernel(AttendArgs a, int R) {
   using T = Ty<BF16>;
-  __shared__ float top[kTileRows], total[kTileRows], acc[kThreads];
+  constexpr int DL = DP / 4, P = kThreads / DL;  // lanes to a row; groups
+  constexpr int kAlone = 16;
+  __shared__ float lse2s[kTileRows], tops[P], totals[P];
+  __shared__ __attribute__((aligned(16))) float acc[kThreads * 4];
   const QLayout& q = a.q;
-  const int tid = threadIdx.x, wave = tid >> 6, l = tid & 63;
-  const int item = blockIdx.x, b = seq_of(a, item), sb = a.b0 + b;
-  const int len = a.len[b], nq = a.tok[b + 1] - a.tok[b], rows = nq * a.G;
+  const int tid = threadIdx.x;
+  const int item = blockIdx.x;
+  const Seq seq = seq_of(a, item);
+  const int b = seq.b, sb = a.b0 + b, len = seq.len, nq = seq.nq, rows = nq * a.G;
   const int nsplit = max(1, (len + a.chunk - 1) / a.chunk);
   const int tiles = (rows + R - 1) / R;
-  const int k = item - a.item[b], h = k / (tiles * nsplit), kk = k - h * tiles * nsplit;
+  const int h = seq.k / (tiles * nsplit), kk = seq.k - h * tiles * nsplit;
   const int tile = tiles - 1 - kk / nsplit, split = kk % nsplit;
   const int r0 = tile * R, nr = min(R, rows - r0);
-  const int64_t first = (int64_t)item - split;
+  const float2* ml = (const float2*)a.ml + ((int64_t)item - split) * R;
 
-  for (int r = wave; r < nr; r += 4) {
-    float m = kLow;
-    for (int s = l; s < nsplit; s += 64) m = fmaxf(m, a.ml[((first + s) * R + r) * 2]);
-    for (int x = 32; x; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
-    float sum = 0.f;
-    for (int s = l; s < nsplit; s += 64)
-      sum += a.ml[((first + s) * R + r) * 2 + 1] * exp2_(a.ml[((first + s) * R + r) * 2] - m);
-    for (int x = 32; x; x >>= 1) sum += __shfl_xor(sum, x);
-    if (l == 0) {
-      top[r] = m;
-      total[r] = sum;
+  if (blockIdx.y == 0) {
+    const bool alone = nsplit <= kAlone;
+    const int group = tid / DL, d = tid % DL * 4, per = alone ? P : 1;
+    for (int rb = split * per; rb < nr; rb += nsplit * per) {
+      const int r = min(alone ? rb + group : rb, nr - 1);
+      const float* part = a.part + (((int64_t)item - split) * R + r) * DP + d;
+      f32x4 v = {0, 0, 0, 0};
+      float top = kLow, total = 0.f;
+#pragma unroll 4
+      for (int s = alone ? 0 : group; s < nsplit; s += alone ? 1 : P) {
+        const float2 x = ml[(int64_t)s * R + r];
+        const f32x4 y = *(const f32x4*)(part + (int64_t)s * R * DP);
+        const float up = fmaxf(top, x.x), f0 = exp2_(top - up), f1 = exp2_(x.x - up);
+        total = total * f0 + x.y * f1;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)  // a split that saw nothing wrote no results
+          v[i] = v[i] * f0 + (x.y != 0.f ? y[i] * f1 : 0.f);
+        top = up;
+      }
+      if (!alone) {
+        __syncthreads();
+        *(f32x4*)(acc + tid * 4) = v;
+        if (d == 0) {
+          tops[group] = top;
+          totals[group] = total;
+        }
+        __syncthreads();
+        if (tid < DL) {
+          for (int p = 1; p < P; ++p) {
+            const float up = fmaxf(top, tops[p]), f0 = exp2_(top - up), f1 = exp2_(tops[p] - up);
+            total = total * f0 + totals[p] * f1;
+            const f32x4 y = *(const f32x4*)(acc + (p * DL + tid) * 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = v[i] * f0 + y[i] * f1;
+            top = up;
+          }
+        }
+      }
+      if (alone ? rb + group >= nr : tid >= DL) continue;
+      const int i = (r0 + r) / a.G, head = h * a.G + (r0 + r - i * a.G);
+      const float inv = total == 0.f ? 0.f : 1.f / total;
+      if (d < q.D)
+        *(u32x2*)((uint16_t*)a.out + (int64_t)(seq.tok + i) * a.o_token +
+                  (int64_t)head * a.o_head + d) =
+            u32x2{T::pack(v[0] * inv, v[1] * inv), T::pack(v[2] * inv, v[3] * inv)};
+      if (d == 0) {
+        const float lse2 = top + __log2f(total);
+        const int64_t row = (int64_t)(seq.tok + i) * a.q_heads + head;
+        if (a.lse)
+          a.lse[(int64_t)a.row0 * a.q_heads + row] = total == 0.f ? -INFINITY : lse2 * kLn2;
+        if (a.row_lse) a.row_lse[row] = total == 0.f ? INFINITY : lse2;
+      }
     }
+    return;
   }
-  __syncthreads();
-  for (int r = split; r < nr; r += nsplit) {
-    constexpr int P = kThreads / DP;  // threads to a dim
-    const int d = tid % DP, i = (r0 + r) / a.G, head = h * a.G + (r0 + r - i * a.G);
-    const float m = top[r], inv = total[r] == 0.f ? 0.f : 1.f / total[r];
-    float v = 0.f;
-    for (int s = tid / DP; s < nsplit; s += P) {
-      const int64_t at = (first + s) * R + r;
-      if (a.ml[at * 2 + 1] != 0.f) v += a.part[at * DP + d] * exp2_(a.ml[at * 2] - m);
+
+  for (int r = tid / 32; r < nr; r += kThreads / 32) {
+    float m = kLow, sum = 0.f;
+    for (int s = tid % 32; s < nsplit; s += 32) {
+      const float2 x = ml[(int64_t)s * R + r];
+      const float up = fmaxf(m, x.x);
+      sum = sum * exp2_(m - up) + x.y * exp2_(x.x - up);
+      m = up;
     }
-    if constexpr (P > 1) {
-      __syncthreads();
-      acc[tid] = v;
-      __syncthreads();
-      if (tid < DP)
-        for (int p = 1; p < P; ++p) v += acc[tid + p * DP];
-    }
-    if (tid < q.D) {
-      const uint32_t w = T::pack(v * inv, 0.f);
-      ((uint16_t*)a.out)[(int64_t)(a.tok[b] + i) * a.o_token + (int64_t)head * a.o_head + d] =
-          (uint16_t)w;
-    }
-    if (tid == 0) {
-      const float lse2 = m + __log2f(total[r]);
-      const int64_t row = (int64_t)(a.tok[b] + i) * a.q_heads + head;
-      if (a.lse)
-        a.lse[(int64_t)a.row0 * a.q_heads + row] = total[r] == 0.f ? -INFINITY : lse2 * kLn2;
-      if (a.row_lse) a.row_lse[row] = total[r] == 0.f ? INFINITY : lse2;
-    }
+    float up = m;
+#pragma unroll
+    for (int x = 16; x; x >>= 1) up = fmaxf(up, __shfl_xor(up, x));
+    sum *= exp2_(m - up);
+#pragma unroll
+    for (int x = 16; x; x >>= 1) sum += __shfl_xor(sum, x);
+    if (tid % 32 == 0) lse2s[r] = sum == 0.f ? INFINITY : up + __log2f(sum);
   }
-  if (!a.weigh || !a.scores) return;
-  for (int r = tid; r < nr; r += kThreads)
-    total[r] = total[r] == 0.f ? INFINITY : top[r] + __log2f(total[r]);
-  __syncthreads();
   const int64_t pitch = (len + 31) & ~31;
   const float* sc = a.scores + (int64_t)a.soff[b] * 32 + (int64_t)h * rows * pitch;
   float* weight = q.weight + (((int64_t)a.layer * q.batch + sb) * q.heads + h) * (int64_t)q.cap;
   const int c0 = split * a.chunk, cn = min(a.chunk, len - c0);
-  for (int t = tid; t < cn; t += kThreads) {
-    float w = 0.f;
+  __syncthreads();
+  for (int t = tid * 4; t < cn; t += kThreads * 4) {  // the scores are padded to 32 tokens
+    f32x4 w = {0, 0, 0, 0};
+#pragma unroll 8
     for (int r = 0; r < nr; ++r) {
-      const float s2 = sc[r * pitch + c0 + t];  // hidden tokens get 0 also where lse is NaN
-      w += s2 == -INFINITY ? 0.f : exp2_(s2 - total[r]);
+      const f32x4 s2 = *(const f32x4*)(sc + r * pitch + c0 + t);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)  // hidden tokens get 0 also where lse is NaN
+        w[i] += s2[i] == -INFINITY ? 0.f : exp2_(s2[i] - lse2s[r]);
     }
-    weight[c0 + t] = a.decay == 0.f ? w : a.decay * weight[c0 + t] + w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (t + i < cn) {
+        float* to = weight + c0 + t + i;
+        *to = a.decay == 0.f ? w[i] : a.decay * *to + w[i];
+      }
   }
 }
 
@@ -848,10 +943,11 @@ __global__ void __launch_bounds__(kThreads) attend_weigh_kernel(AttendArgs a) {
   __shared__ float lse[2][32], slopes[2][32], heres[2][32];
   const QLayout& q = a.q;
   const int tid = threadIdx.x, wave = tid >> 6, l = tid & 63, c = l & 31, hf = l >> 5;
-  const int item = blockIdx.x, b = seq_of(a, item), sb = a.b0 + b;
-  const int len = a.len[b], nq = a.tok[b + 1] - a.tok[b], rows = nq * a.G;
+  const int item = blockIdx.x;
+  const Seq seq = seq_of(a, item);
+  const int b = seq.b, sb = a.b0 + b, len = seq.len, nq = seq.nq, rows = nq * a.G;
   const int tiles = (len + kWeighTokens - 1) / kWeighTokens;
-  const int k = item - a.item[b], h = k / tiles, t0 = (k - h * tiles) * kWeighTokens;
+  const int k = seq.k, h = k / tiles, t0 = (k - h * tiles) * kWeighTokens;
   const int tw = t0 + wave * 32;  // this wave's tokens
 
   const int64_t slab = 2 * (int64_t)a.layer;
@@ -893,7 +989,7 @@ __global__ void __launch_bounds__(kThreads) attend_weigh_kernel(AttendArgs a) {
       const int qi = r / a.G, head = h * a.G + (r - qi * a.G);
       x[i] = u32x4{0, 0, 0, 0};
       if (r < rows && d < q.D)
-        x[i] = *(const u32x4*)((const uint16_t*)a.query + (int64_t)(a.tok[b] + qi) * a.q_token +
+        x[i] = *(const u32x4*)((const uint16_t*)a.query + (int64_t)(seq.tok + qi) * a.q_token +
                                (int64_t)head * a.q_head + d);
     }
     if (tid < 32) {
@@ -901,7 +997,7 @@ __global__ void __launch_bounds__(kThreads) attend_weigh_kernel(AttendArgs a) {
       x_lse = INFINITY;
       x_slope = x_here = 0.f;
       if (r < rows) {
-        x_lse = a.row_lse[(int64_t)(a.tok[b] + qi) * a.q_heads + head];
+        x_lse = a.row_lse[(int64_t)(seq.tok + qi) * a.q_heads + head];
         if (a.slopes && before + qi >= 0) {
           x_slope = a.slopes[head] * kLog2e;
           x_here = (float)(q.position ? q.position[slots + before + qi] : before + qi);
@@ -973,10 +1069,10 @@ __global__ void __launch_bounds__(kThreads) attend_weigh_kernel(AttendArgs a) {
 int padded(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 
 template <typename... More>
-hipError_t launch(const void* fn, uint32_t groups, size_t lds, hipStream_t s, const AttendArgs& a,
+hipError_t launch(const void* fn, dim3 groups, size_t lds, hipStream_t s, const AttendArgs& a,
                   More... more) {
   void* args[] = {const_cast<AttendArgs*>(&a), &more...};
-  return hipLaunchKernel(fn, dim3(groups), dim3(kThreads), args, lds, s);
+  return hipLaunchKernel(fn, groups, dim3(kThreads), args, lds, s);
 }
 
 template <bool BF16, int DP>
@@ -1009,24 +1105,25 @@ const void* pick(const AttendArgs& a, F f) {
 
 hipError_t launch_attend_split(const AttendArgs& a, int rt, bool direct, hipStream_t s) {
   const void* fn = pick(a, [&](auto k) { return decltype(k)::split(rt); });
-  const size_t tables = (size_t)a.chunk * (a.slopes ? 16 : 12);
+  const size_t tables = (size_t)a.chunk * (a.slopes ? 16 : 12) +
+                        (rt > 1 ? (size_t)rt * padded(a.q.D) / 32 * 1024 : 0);
   const size_t join = (size_t)4 * 16 * padded(a.q.D) * 4 + (size_t)4 * rt * 16 * 8;
-  return launch(fn, (uint32_t)a.items, tables > join ? tables : join, s, a, (int)direct);
+  return launch(fn, dim3(a.items), tables > join ? tables : join, s, a, (int)direct);
 }
 
 hipError_t launch_attend_tile(const AttendArgs& a, bool direct, hipStream_t s) {
   const void* fn = pick(a, [](auto k) { return decltype(k)::tile(); });
   const size_t lds = (size_t)2 * kTileTokens * (padded(a.q.D) * 4 + 48) + 264 * 4;
-  return launch(fn, (uint32_t)a.items, lds, s, a, (int)direct);
+  return launch(fn, dim3(a.items), lds, s, a, (int)direct);
 }
 
 hipError_t launch_attend_join(const AttendArgs& a, int rows, hipStream_t s) {
-  return launch(pick(a, [](auto k) { return decltype(k)::join(); }), (uint32_t)a.items, 0, s, a,
-                rows);
+  return launch(pick(a, [](auto k) { return decltype(k)::join(); }),
+                dim3(a.items, a.weigh && a.scores ? 2 : 1), 0, s, a, rows);
 }
 
 hipError_t launch_attend_weigh(const AttendArgs& a, hipStream_t s) {
-  return launch(pick(a, [](auto k) { return decltype(k)::weigh(); }), (uint32_t)a.items, 0, s, a);
+  return launch(pick(a, [](auto k) { return decltype(k)::weigh(); }), dim3(a.items), 0, s, a);
 }
 
 }  // namespace dv

@@ -184,8 +184,16 @@ int plan_of(const Quant& q, const int32_t* q_len, const int32_t* kv_len, const d
   p->split = most <= (p->Dp == 256 ? kFewRowsWide : kFewRows);
   if (p->split) {
     p->R = most <= 16 ? 16 : most <= 32 ? 32 : 64;
+    // The smallest chunk whose work items the card holds all at once.
     const int64_t round = dv::kSplitRound;
-    int64_t chunk = (total / 1536 + round - 1) / round * round;
+    const int64_t slots = 256 * dv::split_groups((int)p->Dp, p->R / 16);
+    int64_t chunk = std::max<int64_t>(1, (total / slots + round - 1) / round) * round;
+    for (; chunk < dv::kSplitChunkMax; chunk += round) {
+      int64_t items = 0;
+      for (int64_t b = 0; b < v.B; ++b)
+        if (q_len[b] > 0) items += std::max<int64_t>(1, (kv_len[b] + chunk - 1) / chunk) * v.H;
+      if (items <= slots) break;
+    }
     if (longest <= 2 * round) chunk = std::max(chunk, (longest + round - 1) / round * round);
     p->chunk = (int32_t)std::min<int64_t>(std::max(chunk, round), dv::kSplitChunkMax);
   } else {

@@ -88,6 +88,10 @@ struct AttendArgs {
 static_assert(sizeof(AttendArgs) <= 3800, "arguments stay under 4 KB");
 // Few rows: RT tiles of 16 rows (1, 2, 4), the token axis split into chunks of
 // a.chunk tokens; `direct`: one chunk a sequence, results go straight to out.
+// Workgroups that a CU holds: registers for as many waves of each SIMD.
+constexpr int split_groups(int DP, int RT) {
+  return RT * DP <= 64 ? 4 : RT * DP <= 128 ? 3 : 2;
+}
 hipError_t launch_attend_split(const AttendArgs& a, int rt, bool direct, hipStream_t s);
 hipError_t launch_attend_join(const AttendArgs& a, int rows, hipStream_t s);
 // Many rows: tiles of kTileRows rows.
