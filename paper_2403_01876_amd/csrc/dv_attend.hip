@@ -145,34 +145,63 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
   return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
 }
 
-// Halves 0 (or 1) of two words, a's below b's.
-__device__ __forceinline__ uint32_t lows(uint32_t a, uint32_t b) {
-  return __builtin_amdgcn_perm(b, a, 0x05040100u);
-}
-__device__ __forceinline__ uint32_t highs(uint32_t a, uint32_t b) {
-  return __builtin_amdgcn_perm(b, a, 0x07060302u);
-}
-
 // ---------------------------------------------------------------------------
 // Few rows (decode steps): a workgroup takes a chunk of one head's tokens, its
 // four waves 32 tokens at a time in turn; 16x16x32 products, queries in RT tiles
-// of 16 columns.  Keys go from memory to the matrix unit in the order they are
-// stored: lane (token l % 16, group l / 16) takes 16 bytes of its token's row.
-// Values: lane (dims (l % 16) * Dp / 16 ..., group g) takes its dims of eight
-// tokens, and the 8 x 8 transposition that the product needs happens in its own
-// registers.  Nothing of the cache passes through LDS.
+// of 16 columns.
+// Each wave copies its own steps' codes from memory to LDS, whole rows at a time
+// and without passing through registers: the next step's keys as soon as these
+// have been read, its values likewise.  No barrier is needed.
+// 16-byte pieces of a row are stored at (piece ^ key(token)), which spreads both
+// kinds of reads over the banks.  Keys are read as the left operand wants them
+// (lane: token l % 16, 16 bytes); values by the transposing read, which gives a
+// lane eight tokens of one dim.
+// Codes become 16-bit numbers as they are, without their scales: a key's scale
+// multiplies its score, a value's its probability, both in 32 bits.  The second
+// product runs in bf16 for either type (codes are exact in it, and so is the
+// range of scaled probabilities), with each probability as the sum of two
+// numbers, which keeps 16 bits of it; the matrix unit has time to spare.
 // Bound by HBM.
 // ---------------------------------------------------------------------------
+// 16 bytes a lane from memory to LDS: to lds + 16 * lane.
+template <bool NT>
+__device__ __forceinline__ void copy_to_lds(const uint8_t* from, uint32_t lds) {
+  if constexpr (NT)
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt"
+                 ::"v"(from), "s"(lds)
+                 : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
+                 ::"v"(from), "s"(lds)
+                 : "memory");
+}
+// Waits until at most N of this wave's accesses to memory are on their way.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+// Waits for this wave's LDS reads.
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+__device__ __forceinline__ u32x2 read_tr8(const uint8_t* p) {
+  typedef int i32x2 __attribute__((ext_vector_type(2)));
+  typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)p));
+}
+
 template <bool BF16, int DP, int RT>
-__global__ void __launch_bounds__(kThreads, split_groups(DP, RT))
+__global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
     attend_split_kernel(AttendArgs a, int direct) {
   using T = Ty<BF16>;
-  constexpr int KL = DP / 64, VW = DP / 64, KS = DP / 32, OJ = DP / 16;
-  constexpr bool kInLds = RT > 1;  // the queries
-  __shared__ int odd[4];
-  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+  using B = Ty<true>;
+  constexpr int CH = DP / 16, KS = DP / 32, OJ = DP / 16;
+  constexpr int kHalf = kSplitStep * DP;  // bytes of a step's keys, or values
+  constexpr bool kInLds = split_queries(DP, RT) > 0;  // the queries
+  constexpr int kLoads = kHalf / 1024;  // copies of a half
+  extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
   const QLayout& q = a.q;
-  const int tid = threadIdx.x, wave = tid >> 6, l = tid & 63, c = l & 15, g = l >> 4;
+  const int tid = threadIdx.x, l = tid & 63, c = l & 15, g = l >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
   const int item = blockIdx.x;
   const Seq seq = seq_of(a, item);
@@ -181,12 +210,16 @@ __global__ void __launch_bounds__(kThreads, split_groups(DP, RT))
   const int h = seq.k / nsplit, c0 = (seq.k - h * nsplit) * a.chunk;
   const int cn = min(a.chunk, len - c0);  // tokens of this chunk
 
-  u32x4* const ql = (u32x4*)lds;  // [RT][KS][lane]
-  float* const tables = (float*)(lds + (kInLds ? RT * KS * 1024 : 0));
+  uint8_t* const kl = lds + wave * 2 * kHalf;
+  uint8_t* const vl = kl + kHalf;
+  u32x4* const ql = (u32x4*)(lds + 8 * kHalf) + l;  // [tile][product][lane]
+  float* const tables = (float*)(lds + 8 * kHalf + split_queries(DP, RT));
   uint32_t* off = (uint32_t*)tables;  // each token's row, in 16 bytes from the head's base
-  float* ks = tables + a.chunk;       // scales; 0: an unmapped block
-  float* vs = tables + 2 * a.chunk;
+  float* ks = tables + a.chunk;       // key scales times the scores' factor; 0: unmapped
+  float* vs = tables + 2 * a.chunk;   // value scales
   float* pos = tables + 3 * a.chunk;
+  f32x4* columns = (f32x4*)(tables + (a.slopes ? 4 : 3) * a.chunk);  // limit, slope, position
+  int* odd = (int*)(columns + RT * 16);
   const int64_t slab = 2 * (int64_t)a.layer;
   const uint8_t* kb = q.codes + slab * q.s_slab + sb * q.s_b + h * q.s_h;
   const uint8_t* vb = kb + q.s_slab;
@@ -209,31 +242,30 @@ __global__ void __launch_bounds__(kThreads, split_groups(DP, RT))
   }
 
   // The queries, and what each column (row c of tile rt) may see.
-  u32x4 qr[kInLds ? 1 : KS];
-  int limit[RT];
-  float slope[RT], here[RT];
+  u32x4 qr[kInLds ? 1 : RT][KS];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const int r = rt * 16 + c, i = r / a.G, head = h * a.G + (r - i * a.G);
     const bool on = r < rows;
-    if (!kInLds || (rt & 3) == wave || RT < 4) {
-      const uint16_t* src = (const uint16_t*)a.query +
-                            (int64_t)(on ? seq.tok + i : 0) * a.q_token + (int64_t)head * a.q_head;
+    const uint16_t* src = (const uint16_t*)a.query +
+                          (int64_t)(on ? seq.tok + i : 0) * a.q_token + (int64_t)head * a.q_head;
+    const bool mine = rt % 4 == wave;  // what goes to LDS is one wave's to read
 #pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        const int d = (s >> 1) * 64 + g * 16 + (s & 1) * 8;
-        const u32x4 x = on && d < q.D ? *(const u32x4*)(src + d) : u32x4{0, 0, 0, 0};
-        if constexpr (kInLds)
-          ql[(rt * KS + s) * 64 + l] = x;
-        else
-          qr[s] = x;
-      }
+    for (int s = 0; s < KS; ++s) {
+      const int d = (s >> 1) * 64 + g * 16 + (s & 1) * 8;
+      const u32x4 x = on && d < q.D && (!kInLds || mine) ? *(const u32x4*)(src + d)
+                                                         : u32x4{0, 0, 0, 0};
+      if constexpr (!kInLds) qr[rt][s] = x;
+      if (kInLds && mine) ql[(rt * KS + s) * 64] = x;
     }
-    limit[rt] = on ? len - nq + i : -1;
-    slope[rt] = here[rt] = 0.f;
-    if (a.slopes && on && limit[rt] >= 0) {
-      slope[rt] = a.slopes[head] * kLog2e;
-      here[rt] = (float)(q.position ? q.position[slots + limit[rt]] : limit[rt]);
+    if (mine && g == 0) {
+      const int limit = on ? len - nq + i : -1;
+      float slope = 0.f, here = 0.f;
+      if (a.slopes && limit >= 0) {
+        slope = a.slopes[head] * kLog2e;
+        here = (float)(q.position ? q.position[slots + limit] : limit);
+      }
+      columns[r] = f32x4{__int_as_float(limit), slope, here, 0.f};
     }
   }
   // (LDS is all that the workgroup shares so far: loads may stay in flight)
@@ -243,41 +275,32 @@ __global__ void __launch_bounds__(kThreads, split_groups(DP, RT))
   const bool holes = odd[0] | odd[1] | odd[2] | odd[3];
   const int all_see = len - nq;  // slots up to this one are seen by every row
 
-  const int kd = g * 16, vd = c * (DP / 16);
-  const bool pad = q.D < DP;
-  // One set of registers holds the step's codes: the next step's keys are asked
-  // for as soon as the products have read these, its values likewise, so loads
-  // are in flight all the time at no cost in registers.
-  u32x4 kx[2][KL];
-  uint32_t vx[8][VW];
-  auto load_k = [&](int t) {
+  // Copy n of a half: tokens n * 64 / CH ..., lane's token l / CH of them, piece
+  // l % CH of its place.  Pieces past head_dim repeat the row's first one: they
+  // meet zeros of the queries, or make dims that are not written.
+  auto key_of = [](int tok) { return tok / (16 / CH) & (CH - 1); };
+  const uint32_t k_to = __builtin_amdgcn_readfirstlane(
+      (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)kl);
+  uint32_t piece[kLoads];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const uint8_t* p = kb + (uint64_t)off[t + u * 16 + c] * 16;
+  for (int n = 0; n < kLoads; ++n) {
+    piece[n] = (l % CH) ^ key_of(n * (64 / CH) + l / CH);
+    piece[n] = (int)piece[n] * 16 < q.D ? piece[n] : 0;
+  }
+  auto fetch = [&](const uint8_t* from, uint32_t to, int t) {
+    const uint32_t* row = off + t + l / CH;
+    uint32_t at[kLoads];
 #pragma unroll
-      for (int i = 0; i < KL; ++i)
-        kx[u][i] = *(const u32x4*)(p + (pad && kd + 64 * i >= q.D ? 0 : kd + 64 * i));
-    }
-  };
-  auto load_v = [&](int t) {
+    for (int n = 0; n < kLoads; ++n) at[n] = row[n * (64 / CH)] + piece[n];
+    wait_lds();
+    if (a.nt) {
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const u32x4 o = *(const u32x4*)(off + t + u * 16 + g * 4);
+      for (int n = 0; n < kLoads; ++n)
+        copy_to_lds<true>(from + (uint64_t)at[n] * 16, to + n * 1024);
+    } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint8_t* p = vb + (uint64_t)o[i] * 16 + (pad && vd >= q.D ? 0 : vd);
-        if constexpr (VW == 1) vx[u * 4 + i][0] = *(const uint32_t*)p;
-        if constexpr (VW == 2) {
-          const u32x2 w = *(const u32x2*)p;
-          vx[u * 4 + i][0] = w[0];
-          vx[u * 4 + i][1] = w[1];
-        }
-        if constexpr (VW == 4) {
-          const u32x4 w = *(const u32x4*)p;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) vx[u * 4 + i][e] = w[e];
-        }
-      }
+      for (int n = 0; n < kLoads; ++n)
+        copy_to_lds<false>(from + (uint64_t)at[n] * 16, to + n * 1024);
     }
   };
 
@@ -291,76 +314,93 @@ __global__ void __launch_bounds__(kThreads, split_groups(DP, RT))
     for (int j = 0; j < OJ; ++j) o[rt][j] = f32x4{0, 0, 0, 0};
   }
   const int64_t pitch = (len + 31) & ~31;
+  // where this lane reads: its keys' row, and its row of a transposed read
+  const int krow = c * DP, kkey = key_of(c);
+  const int vtok = (l & 15) >> 1, vrow = (vtok < 4 ? g * 4 + vtok : 12 + g * 4 + vtok);
+  const int vkey = key_of(vrow);
+  const uint8_t* const vread = vl + vrow * DP + (l & 1) * 8;
 
-  auto step = [&](int t, auto more) {
+  // Stores count as accesses on their way, in order: none before the wait for the
+  // values, unless the scores' registers are wanted.
+  constexpr bool kLate = RT == 1;
+  auto store_scores = [&](f32x4 (&s)[RT][2], int first) {
+    if (!a.weigh) return;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      if (rt * 16 + c >= rows) continue;
+      float* to = a.scores + (int64_t)a.soff[b] * 32 +
+                  ((int64_t)h * rows + rt * 16 + c) * pitch + first;
+      *(f32x4*)to = s[rt][0];
+      *(f32x4*)(to + 16) = s[rt][1];
+    }
+  };
+  auto step = [&](int t, bool more) {
+    wait_loads<kLoads>();  // the keys; the values may still come
     f32x4 s[RT][2];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) s[rt][0] = s[rt][1] = f32x4{0, 0, 0, 0};
-    const float scale[2] = {ks[t + c], ks[t + 16 + c]};
 #pragma unroll
-    for (int i = 0; i < KL; ++i)
+    for (int i = 0; i < KS / 2; ++i) {
+      u32x4 x[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)  // 16 tokens on the key is the same
+        x[u] = *(const u32x4*)(kl + u * 16 * DP + krow + (((g + 4 * i) ^ kkey) << 4));
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         u32x4 y[2];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          u32x2 w = {kx[u][i][2 * e], kx[u][i][2 * e + 1]};
-          if (pad && kd + 64 * i >= q.D) w = u32x2{0, 0};
-          y[u] = u32x4{T::template cvt<false>(w[0], scale[u]), T::template cvt<true>(w[0], scale[u]),
-                       T::template cvt<false>(w[1], scale[u]), T::template cvt<true>(w[1], scale[u])};
-        }
+        for (int u = 0; u < 2; ++u)
+          y[u] = u32x4{T::template cvt<false>(x[u][2 * e], 1.f), T::template cvt<true>(x[u][2 * e], 1.f),
+                       T::template cvt<false>(x[u][2 * e + 1], 1.f),
+                       T::template cvt<true>(x[u][2 * e + 1], 1.f)};
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-          const u32x4 x = kInLds ? ql[(rt * KS + 2 * i + e) * 64 + l] : qr[kInLds ? 0 : 2 * i + e];
-          s[rt][0] = T::mma16(y[0], x, s[rt][0]);
-          s[rt][1] = T::mma16(y[1], x, s[rt][1]);
+          const u32x4 z = kInLds ? ql[(rt * KS + 2 * i + e) * 64] : qr[kInLds ? 0 : rt][2 * i + e];
+          s[rt][0] = T::mma16(y[0], z, s[rt][0]);
+          s[rt][1] = T::mma16(y[1], z, s[rt][1]);
         }
       }
-    if constexpr (decltype(more)::value) load_k(t + kSplitRound);
+    }
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       settle(s[rt][0]);
       settle(s[rt][1]);
     }
+    if (more) fetch(kb, k_to, t + kSplitRound);
     const int first = c0 + t + g * 4;  // this lane's tokens: first + 16 u + r
     const bool mask = holes || c0 + t + kSplitStep - 1 > all_see;
+    const f32x4 kscale[2] = {*(const f32x4*)(ks + t + g * 4), *(const f32x4*)(ks + t + 16 + g * 4)};
     uint32_t seen[RT];  // bit u * 4 + r
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u) s[rt][u] = s[rt][u] * a.scale2;
+      for (int u = 0; u < 2; ++u) s[rt][u] = s[rt][u] * kscale[u];
       if (a.slopes) {
+        const f32x4 column = columns[rt * 16 + c];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           const f32x4 at = *(const f32x4*)(pos + t + u * 16 + g * 4);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) s[rt][u][r] += slope[rt] * (at[r] - here[rt]);
+          for (int r = 0; r < 4; ++r) s[rt][u][r] += column[1] * (at[r] - column[2]);
         }
       }
       if (mask) {
+        const int limit = __float_as_int(columns[rt * 16 + c][0]);
         seen[rt] = 0;
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const f32x4 there = *(const f32x4*)(ks + t + u * 16 + g * 4);
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const bool sees = first + u * 16 + r <= limit[rt] && there[r] != 0.f;
+            const bool sees = first + u * 16 + r <= limit && kscale[u][r] != 0.f;
             s[rt][u][r] = sees ? s[rt][u][r] : -INFINITY;
             seen[rt] |= (uint32_t)sees << (u * 4 + r);
           }
-        }
-      }
-      if (a.weigh && rt * 16 + c < rows) {
-        float* to = a.scores + (int64_t)a.soff[b] * 32 +
-                    ((int64_t)h * rows + rt * 16 + c) * pitch + first;
-        *(f32x4*)to = s[rt][0];
-        *(f32x4*)(to + 16) = s[rt][1];
       }
       float most = s[rt][0][0];
 #pragma unroll
       for (int i = 1; i < 8; ++i) most = fmaxf(most, s[rt][i >> 2][i & 3]);
-      if (__any(most > m[rt] + (kSlack + T::kLift))) {
-        float up = fmaxf(most - T::kLift, m[rt]);
+      if (__any(most > m[rt] + kSlack)) {
+        float up = fmaxf(most, m[rt]);
         up = fmaxf(up, __shfl_xor(up, 16));
         up = fmaxf(up, __shfl_xor(up, 32));
         const float f = exp2_(m[rt] - up);
@@ -370,108 +410,102 @@ __global__ void __launch_bounds__(kThreads, split_groups(DP, RT))
         for (int j = 0; j < OJ; ++j) o[rt][j] = o[rt][j] * f;
       }
     }
-    // Probabilities as the sum of two 16-bit numbers: the matrix unit has time
-    // to spare here, and the results keep 32-bit accuracy.
+    if (!kLate) store_scores(s, first);
+    const f32x4 vscale[2] = {*(const f32x4*)(vs + t + g * 4), *(const f32x4*)(vs + t + 16 + g * 4)};
     u32x4 hi[RT], lo[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float p0 = exp2_(s[rt][i >> 1][(2 * i) & 3] - m[rt]);
-        const float p1 = exp2_(s[rt][i >> 1][(2 * i + 1) & 3] - m[rt]);
+        const int u = i >> 1, r = (2 * i) & 3;
+        float p0 = exp2_(s[rt][u][r] - m[rt]), p1 = exp2_(s[rt][u][r + 1] - m[rt]);
         sum[rt] += p0 + p1;
-        hi[rt][i] = T::pack(p0, p1);
-        lo[rt][i] = T::pack(p0 - T::lo(hi[rt][i]), p1 - T::hi(hi[rt][i]));
+        p0 *= vscale[u][r];
+        p1 *= vscale[u][r + 1];
+        hi[rt][i] = B::pack(p0, p1);
+        lo[rt][i] = B::pack(p0 - B::lo(hi[rt][i]), p1 - B::hi(hi[rt][i]));
       }
     }
+    if (more && (kLate || !a.weigh))
+      wait_loads<kLoads>();  // the values; the next keys may still come
+    else
+      wait_loads<0>();
     if (mask) {
-      // A NaN value reaches the queries that see its token and no others: it
-      // leaves the product below, and where a product of "is NaN" and "is seen"
-      // is not zero the result is NaN.
+      // A NaN value reaches the queries that see its token and no others: where
+      // the product of "is NaN" and "is seen" is not zero the result is NaN, and
+      // the codes become zeros.
       uint32_t any = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
+      for (int n = 0; n < kLoads; ++n) {
+        const u32x4 w = *(const u32x4*)(vl + n * 1024 + l * 16);
 #pragma unroll
-        for (int w = 0; w < VW; ++w) any |= nan_bytes(vx[i][w]);
+        for (int e = 0; e < 4; ++e) any |= nan_bytes(w[e]);
+      }
       if (__any(any != 0)) {
 #pragma unroll
-        for (int w = 0; w < VW; ++w) {
-          uint32_t is[8][2];
+        for (int j = 0; j < OJ; ++j) {
+          const u32x2 w = read_tr8(vread + ((j ^ vkey) << 4));
+          u32x4 is;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const uint32_t n = nan_bytes(vx[i][w]) >> 7;
-            is[i][0] = (n & 1) * T::kOne | ((n >> 8) & 1) * (T::kOne << 16);
-            is[i][1] = ((n >> 16) & 1) * T::kOne | ((n >> 24) & 1) * (T::kOne << 16);
-            vx[i][w] &= ~(n * 0xffu);
+          for (int e = 0; e < 2; ++e) {
+            const uint32_t n = nan_bytes(w[e]) >> 7;
+            is[2 * e] = (n & 1) * B::kOne | ((n >> 8) & 1) * (B::kOne << 16);
+            is[2 * e + 1] = ((n >> 16) & 1) * B::kOne | ((n >> 24) & 1) * (B::kOne << 16);
           }
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt) {
             u32x4 sees;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              sees[i] = ((seen[rt] >> (2 * i)) & 1) * T::kOne |
-                        ((seen[rt] >> (2 * i + 1)) & 1) * (T::kOne << 16);
+              sees[i] = ((seen[rt] >> (2 * i)) & 1) * B::kOne |
+                        ((seen[rt] >> (2 * i + 1)) & 1) * (B::kOne << 16);
+            f32x4 z = B::mma16(is, sees, f32x4{0, 0, 0, 0});
+            settle(z);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              u32x4 y;
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                y[i] = e & 1 ? highs(is[2 * i][e >> 1], is[2 * i + 1][e >> 1])
-                             : lows(is[2 * i][e >> 1], is[2 * i + 1][e >> 1]);
-              const f32x4 z = T::mma16(y, sees, f32x4{0, 0, 0, 0});
-#pragma unroll
-              for (int r = 0; r < 4; ++r)
-                o[rt][4 * w + e][r] = z[r] > 0.f ? NAN : o[rt][4 * w + e][r];
-            }
+            for (int r = 0; r < 4; ++r) o[rt][j][r] = z[r] > 0.f ? NAN : o[rt][j][r];
           }
         }
+        wait_lds();
+#pragma unroll
+        for (int n = 0; n < kLoads; ++n) {
+          u32x4* at = (u32x4*)(vl + n * 1024 + l * 16);
+          u32x4 w = *at;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[e] &= ~((nan_bytes(w[e]) >> 7) * 0xffu);
+          *at = w;
+        }
+        wait_lds();
       }
     }
-    const f32x4 v0 = *(const f32x4*)(vs + t + g * 4), v1 = *(const f32x4*)(vs + t + 16 + g * 4);
+    u32x2 w[OJ];
 #pragma unroll
-    for (int w = 0; w < VW; ++w)
+    for (int j = 0; j < OJ; ++j) w[j] = read_tr8(vread + ((j ^ vkey) << 4));
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {  // dims 0, 1 and 2, 3 of the word
-        uint32_t y[8];
+    for (int j = 0; j < OJ; ++j) {
+      const u32x4 v = {B::cvt<false>(w[j][0], 1.f), B::cvt<true>(w[j][0], 1.f),
+                       B::cvt<false>(w[j][1], 1.f), B::cvt<true>(w[j][1], 1.f)};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float scale = i < 4 ? v0[i] : v1[i & 3];
-          y[i] = half ? T::template cvt<true>(vx[i][w], scale)
-                      : T::template cvt<false>(vx[i][w], scale);
-        }
+      for (int rt = 0; rt < RT; ++rt) o[rt][j] = B::mma16(v, hi[rt], o[rt][j]);
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          u32x4 v;
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            v[i] = e ? highs(y[2 * i], y[2 * i + 1]) : lows(y[2 * i], y[2 * i + 1]);
-          const int j = 4 * w + 2 * half + e;
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt) {
-            o[rt][j] = T::mma16(v, hi[rt], o[rt][j]);
-            o[rt][j] = T::mma16(v, lo[rt], o[rt][j]);
-          }
-        }
-      }
-    if constexpr (decltype(more)::value) load_v(t + kSplitRound);
+      for (int rt = 0; rt < RT; ++rt) o[rt][j] = B::mma16(v, lo[rt], o[rt][j]);
+    }
+    if (kLate) store_scores(s, first);
+    if (more) fetch(vb, k_to + kHalf, t + kSplitRound);
   };
 
   int t = wave * kSplitStep;
   if (t < cn) {
-    load_k(t);
-    load_v(t);
+    fetch(kb, k_to, t);
+    fetch(vb, k_to + kHalf, t);
   }
   // The scales follow the first codes: both are on their way at once.
   for (int i = tid; i < ((cn + kSplitStep - 1) & -kSplitStep); i += kThreads) {
     const int blk = ((const int*)ks)[i];
-    ks[i] = blk < 0 ? 0.f : sk[blk * q.c_blk];
+    ks[i] = blk < 0 ? 0.f : sk[blk * q.c_blk] * a.scale2;
     vs[i] = sk[max(blk, 0) * q.c_blk + q.c_slab];
   }
   lds_barrier();
-  if (t < cn) {
-    for (; t + kSplitRound < cn; t += kSplitRound) step(t, std::true_type{});
-    step(t, std::false_type{});
-  }
+  for (; t < cn; t += kSplitRound) step(t, t + kSplitRound < cn);
 
   // Join the four waves.
   __syncthreads();  // the tables are done with
@@ -493,16 +527,13 @@ __global__ void __launch_bounds__(kThreads, split_groups(DP, RT))
     float most = kLow;
     for (int w = 0; w < 4; ++w) most = fmaxf(most, mls[(w * RT * 16 + rt * 16 + c) * 2]);
     const float f = exp2_(m[rt] - most);
+    if (rt * 16 + c < rows)
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-#pragma unroll
-      for (int j = 0; j < OJ; j += 4)
-        *(f32x4*)(sums + (wave * 16 + c) * DP + (g * 4 + r) * OJ + j) =
-            f32x4{o[rt][j][r] * f, o[rt][j + 1][r] * f, o[rt][j + 2][r] * f, o[rt][j + 3][r] * f};
+      for (int j = 0; j < OJ; ++j)  // dims 16 j + 4 g ...
+        *(f32x4*)(sums + (wave * 16 + c) * DP + j * 16 + g * 4) = o[rt][j] * f;
     __syncthreads();
-    for (int e = tid * 4; e < 16 * DP; e += kThreads * 4) {
+    for (int e = tid * 4; e < min(16, rows - rt * 16) * DP; e += kThreads * 4) {
       const int rr = e / DP, d = e % DP, r = rt * 16 + rr;
-      if (r >= rows) continue;
       f32x4 v = *(const f32x4*)(sums + e);
 #pragma unroll
       for (int w = 1; w < 4; ++w) v += *(const f32x4*)(sums + w * 16 * DP + e);
@@ -1066,8 +1097,6 @@ __global__ void __launch_bounds__(kThreads) attend_weigh_kernel(AttendArgs a) {
   }
 }
 
-int padded(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
-
 template <typename... More>
 hipError_t launch(const void* fn, dim3 groups, size_t lds, hipStream_t s, const AttendArgs& a,
                   More... more) {
@@ -1105,10 +1134,8 @@ const void* pick(const AttendArgs& a, F f) {
 
 hipError_t launch_attend_split(const AttendArgs& a, int rt, bool direct, hipStream_t s) {
   const void* fn = pick(a, [&](auto k) { return decltype(k)::split(rt); });
-  const size_t tables = (size_t)a.chunk * (a.slopes ? 16 : 12) +
-                        (rt > 1 ? (size_t)rt * padded(a.q.D) / 32 * 1024 : 0);
-  const size_t join = (size_t)4 * 16 * padded(a.q.D) * 4 + (size_t)4 * rt * 16 * 8;
-  return launch(fn, dim3(a.items), tables > join ? tables : join, s, a, (int)direct);
+  return launch(fn, dim3(a.items), split_lds(padded(a.q.D), rt, a.chunk, a.slopes != nullptr), s, a,
+                (int)direct);
 }
 
 hipError_t launch_attend_tile(const AttendArgs& a, bool direct, hipStream_t s) {

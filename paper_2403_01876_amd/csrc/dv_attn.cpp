@@ -180,19 +180,19 @@ int plan_of(const Quant& q, const int32_t* q_len, const int32_t* kv_len, const d
   }
   // rows are counted in 32 bits
   if (most >= (1ll << 30) || tokens * a->q_heads >= (1ll << 31)) return DV_ERR_UNSUPPORTED;
-  p->Dp = v.D <= 64 ? 64 : v.D <= 128 ? 128 : 256;
+  p->Dp = dv::padded(v.D);
   p->split = most <= (p->Dp == 256 ? kFewRowsWide : kFewRows);
   if (p->split) {
     p->R = most <= 16 ? 16 : most <= 32 ? 32 : 64;
     // The smallest chunk whose work items the card holds all at once.
     const int64_t round = dv::kSplitRound;
-    const int64_t slots = 256 * dv::split_groups((int)p->Dp, p->R / 16);
-    int64_t chunk = std::max<int64_t>(1, (total / slots + round - 1) / round) * round;
+    int64_t chunk = std::max<int64_t>(1, total / 1024 / round) * round;
     for (; chunk < dv::kSplitChunkMax; chunk += round) {
       int64_t items = 0;
       for (int64_t b = 0; b < v.B; ++b)
         if (q_len[b] > 0) items += std::max<int64_t>(1, (kv_len[b] + chunk - 1) / chunk) * v.H;
-      if (items <= slots) break;
+      if (items <= 256 * dv::split_groups((int)p->Dp, p->R / 16, (int)chunk, a->slopes != nullptr))
+        break;
     }
     if (longest <= 2 * round) chunk = std::max(chunk, (longest + round - 1) / round * round);
     p->chunk = (int32_t)std::min<int64_t>(std::max(chunk, round), dv::kSplitChunkMax);
@@ -318,6 +318,13 @@ int attend(const dv_quant* c, int32_t mb, int32_t layer, const int32_t* q_len,
   a.chunk = p.chunk;
   a.weigh = u->weigh != 0;
   a.bf16 = u->type == DV_BF16;
+  // Codes of 96 MB and more do not stay in the last-level cache, and are read
+  // faster past it: 138 MB 36.1 us instead of 40.9, 268 MB 79.2 instead of 87.2,
+  // but 63 MB 24.5 instead of 23.5.
+  int64_t codes = 0;
+  for (int64_t b = 0; b < v.B; ++b)
+    if (q_len[b] > 0) codes += kv_len[b] * v.H * D * 2;
+  a.nt = codes >= 96 << 20;
   int64_t row0 = 0;
   for (int64_t b0 = 0; b0 < v.B; b0 += kQSeqs) {
     const int nseq = (int)std::min<int64_t>(kQSeqs, v.B - b0);
@@ -427,11 +434,19 @@ int dv_attend_bytes(const dv_quant* c, const int32_t* q_len, const int32_t* kv_l
   Quant q;
   int rc = layout8(c, &q);
   if (rc != DV_OK) return rc;
-  Plan p;
-  rc = plan_of(q, q_len, kv_len, a, &p);
-  if (rc != DV_OK) return rc;
-  if (!out_bytes) return DV_ERR_INVALID;
-  *out_bytes = p.bytes;
+  if (!a || !out_bytes) return DV_ERR_INVALID;
+  // With and without slopes, whose tables in LDS make other splits best.
+  static const float slope = 0.f;
+  uint64_t most = 0;
+  for (int i = 0; i < 2; ++i) {
+    dv_attend_args x = *a;
+    x.slopes = i ? &slope : nullptr;
+    Plan p;
+    rc = plan_of(q, q_len, kv_len, &x, &p);
+    if (rc != DV_OK) return rc;
+    most = std::max(most, p.bytes);
+  }
+  *out_bytes = most;
   return DV_OK;
 }
 

@@ -80,6 +80,7 @@ struct AttendArgs {
   int32_t layer, b0, nseq, items;
   int32_t G, q_heads, chunk;  // chunk: tokens of a split (rows of a tile where there are many)
   int32_t weigh, bf16, row0;  // row0: rows of q before this launch's
+  int32_t nt, pad;            // whether the codes are read past the caches
   int32_t item[kQSeqs];       // work items of earlier sequences; INT32_MAX past the last
   int32_t tok[kQSeqs + 1];    // queries of earlier sequences
   int32_t len[kQSeqs];        // tokens in the cache
@@ -88,9 +89,30 @@ struct AttendArgs {
 static_assert(sizeof(AttendArgs) <= 3800, "arguments stay under 4 KB");
 // Few rows: RT tiles of 16 rows (1, 2, 4), the token axis split into chunks of
 // a.chunk tokens; `direct`: one chunk a sequence, results go straight to out.
-// Workgroups that a CU holds: registers for as many waves of each SIMD.
-constexpr int split_groups(int DP, int RT) {
-  return RT * DP <= 64 ? 4 : RT * DP <= 128 ? 3 : 2;
+// head_dim as the kernels are built for it.
+inline int padded(int64_t D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
+// Tokens of a wave's step over the cache, and of a workgroup's (four waves).
+constexpr int kSplitStep = 32;
+constexpr int kSplitRound = 4 * kSplitStep;
+constexpr int kSplitChunkMax = 1792;
+// Bytes of LDS for the queries of the split kernel: those of four tiles leave no
+// registers for two workgroups a CU.
+constexpr int split_queries(int DP, int RT) { return RT == 4 ? RT * DP * 32 : 0; }
+// Workgroups of the split kernel that the registers of RT tiles of results allow
+// a CU, its bytes of LDS (the codes of a step of four waves and the tables of a
+// chunk, or the waves' results) and those that both allow.
+constexpr int split_waves(int DP, int RT) {
+  return DP <= 64 ? (RT == 1 ? 4 : RT == 2 ? 3 : 2) : DP <= 128 ? (RT == 1 ? 3 : 2) : 1;
+}
+inline size_t split_lds(int DP, int rt, int chunk, bool slopes) {
+  const size_t tables = (size_t)4 * 2 * kSplitStep * DP + split_queries(DP, rt) +
+                        (size_t)chunk * (slopes ? 16 : 12) + rt * 256 + 16;
+  const size_t join = (size_t)4 * 16 * DP * 4 + (size_t)4 * rt * 16 * 8;
+  return tables > join ? tables : join;
+}
+inline int split_groups(int DP, int rt, int chunk, bool slopes) {
+  const int by_lds = (int)(160 * 1024 / split_lds(DP, rt, chunk, slopes));
+  return by_lds < split_waves(DP, rt) ? by_lds : split_waves(DP, rt);
 }
 hipError_t launch_attend_split(const AttendArgs& a, int rt, bool direct, hipStream_t s);
 hipError_t launch_attend_join(const AttendArgs& a, int rows, hipStream_t s);
@@ -100,11 +122,6 @@ hipError_t launch_attend_tile(const AttendArgs& a, bool direct, hipStream_t s);
 // Column sums of the probabilities, from the rows' lse.
 constexpr int kWeighTokens = 128;
 hipError_t launch_attend_weigh(const AttendArgs& a, hipStream_t s);
-
-// Tokens of a wave's step over the cache, and of a workgroup's (four waves).
-constexpr int kSplitStep = 32;
-constexpr int kSplitRound = 4 * kSplitStep;
-constexpr int kSplitChunkMax = 2048;
 
 // ---- dv_evict ----
 struct EvictArgs {
