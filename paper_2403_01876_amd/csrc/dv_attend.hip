@@ -122,6 +122,9 @@ __device__ __forceinline__ Seq seq_of(const AttendArgs& a, int item) {
   return q;
 }
 
+// A value known to be the same in all lanes, as a scalar (quotients are not seen to be).
+__device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
 // Called on products' results before any branch: ends the wait for them in the
 // block of the products.  Left to itself, the compiler (ROCm 7.2) counts the wait
 // states between a product and the first read of its result along one path only
@@ -143,6 +146,32 @@ __device__ __forceinline__ void lds_barrier() {
 // 0x80 in each byte of w that is a NaN code.
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
   return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+}
+
+// NaN values of tokens that are hidden from some rows leave the products (as
+// zeros), since 0 times NaN is NaN.  Once the results are written this makes NaN
+// of those that they belong to: rows [r0, r0 + nr) that see such a token of
+// [from, to).  `part`: sums of a split (rows of DP), or null: the call's results.
+__device__ __forceinline__ void spread_nan(const AttendArgs& a, int sb, int h, int len, int nq,
+                                        int tok, int from, int to, int r0, int nr, float* part,
+                                        int DP) {
+  const QLayout& q = a.q;
+  const uint8_t* vb = q.codes + (2 * (int64_t)a.layer + 1) * q.s_slab + sb * q.s_b + h * q.s_h;
+  for (int x = threadIdx.x; x < nr * q.D; x += kThreads) {
+    const int r = x / q.D, d = x - r * q.D, i = (r0 + r) / a.G, head = h * a.G + r0 + r - i * a.G;
+    bool nan = false;
+    for (int t = from; t < min(to, len - nq + i + 1); ++t) {
+      const int j = q.d_bs.div(t);
+      const int64_t blk = q.bt ? q.bt[(int64_t)sb * q.max_blocks + j] : j;
+      if (q.bt && (uint64_t)blk >= (uint64_t)q.num_blocks) continue;
+      nan |= (vb[blk * q.s_blk + (int64_t)(t - j * q.bs) * q.D + d] & 127) == 127;
+    }
+    if (!nan) continue;
+    if (part)
+      part[(int64_t)r * DP + d] = NAN;
+    else
+      ((uint16_t*)a.out)[(int64_t)(tok + i) * a.o_token + (int64_t)head * a.o_head + d] = 0x7fff;
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -206,8 +235,8 @@ __global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
   const int item = blockIdx.x;
   const Seq seq = seq_of(a, item);
   const int b = seq.b, sb = a.b0 + b, len = seq.len, nq = seq.nq, rows = nq * a.G;
-  const int nsplit = max(1, (len + a.chunk - 1) / a.chunk);
-  const int h = seq.k / nsplit, c0 = (seq.k - h * nsplit) * a.chunk;
+  const int nsplit = max(1, scalar((len + a.chunk - 1) / a.chunk));
+  const int h = scalar(seq.k / nsplit), c0 = (seq.k - h * nsplit) * a.chunk;
   const int cn = min(a.chunk, len - c0);  // tokens of this chunk
 
   uint8_t* const kl = lds + wave * 2 * kHalf;
@@ -215,7 +244,7 @@ __global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
   u32x4* const ql = (u32x4*)(lds + 8 * kHalf) + l;  // [tile][product][lane]
   float* const tables = (float*)(lds + 8 * kHalf + split_queries(DP, RT));
   uint32_t* off = (uint32_t*)tables;  // each token's row, in 16 bytes from the head's base
-  float* ks = tables + a.chunk;       // key scales times the scores' factor; 0: unmapped
+  float* ks = tables + a.chunk;       // key scales times the scores' factor; NaN: unmapped
   float* vs = tables + 2 * a.chunk;   // value scales
   float* pos = tables + 3 * a.chunk;
   f32x4* columns = (f32x4*)(tables + (a.slopes ? 4 : 3) * a.chunk);  // limit, slope, position
@@ -314,6 +343,7 @@ __global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
     for (int j = 0; j < OJ; ++j) o[rt][j] = f32x4{0, 0, 0, 0};
   }
   const int64_t pitch = (len + 31) & ~31;
+  int nan_from = INT32_MAX, nan_to = 0;  // where values became zeros (spread_nan)
   // where this lane reads: its keys' row, and its row of a transposed read
   const int krow = c * DP, kkey = key_of(c);
   const int vtok = (l & 15) >> 1, vrow = (vtok < 4 ? g * 4 + vtok : 12 + g * 4 + vtok);
@@ -370,7 +400,6 @@ __global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
     const int first = c0 + t + g * 4;  // this lane's tokens: first + 16 u + r
     const bool mask = holes || c0 + t + kSplitStep - 1 > all_see;
     const f32x4 kscale[2] = {*(const f32x4*)(ks + t + g * 4), *(const f32x4*)(ks + t + 16 + g * 4)};
-    uint32_t seen[RT];  // bit u * 4 + r
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
 #pragma unroll
@@ -386,14 +415,12 @@ __global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
       }
       if (mask) {
         const int limit = __float_as_int(columns[rt * 16 + c][0]);
-        seen[rt] = 0;
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const bool sees = first + u * 16 + r <= limit && kscale[u][r] != 0.f;
+            const bool sees = first + u * 16 + r <= limit && kscale[u][r] == kscale[u][r];
             s[rt][u][r] = sees ? s[rt][u][r] : -INFINITY;
-            seen[rt] |= (uint32_t)sees << (u * 4 + r);
           }
       }
       float most = s[rt][0][0];
@@ -431,51 +458,26 @@ __global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
     else
       wait_loads<0>();
     if (mask) {
-      // A NaN value reaches the queries that see its token and no others: where
-      // the product of "is NaN" and "is seen" is not zero the result is NaN, and
-      // the codes become zeros.
       uint32_t any = 0;
 #pragma unroll
       for (int n = 0; n < kLoads; ++n) {
-        const u32x4 w = *(const u32x4*)(vl + n * 1024 + l * 16);
+        u32x4* const at = (u32x4*)(vl + n * 1024 + l * 16);
+        u32x4 w = *at;
+        uint32_t nan = 0;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) any |= nan_bytes(w[e]);
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t x = nan_bytes(w[e]);
+          nan |= x;
+          w[e] &= ~((x >> 7) * 0xffu);
+        }
+        if (nan) *at = w;
+        any |= nan;
       }
       if (__any(any != 0)) {
-#pragma unroll
-        for (int j = 0; j < OJ; ++j) {
-          const u32x2 w = read_tr8(vread + ((j ^ vkey) << 4));
-          u32x4 is;
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const uint32_t n = nan_bytes(w[e]) >> 7;
-            is[2 * e] = (n & 1) * B::kOne | ((n >> 8) & 1) * (B::kOne << 16);
-            is[2 * e + 1] = ((n >> 16) & 1) * B::kOne | ((n >> 24) & 1) * (B::kOne << 16);
-          }
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt) {
-            u32x4 sees;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              sees[i] = ((seen[rt] >> (2 * i)) & 1) * B::kOne |
-                        ((seen[rt] >> (2 * i + 1)) & 1) * (B::kOne << 16);
-            f32x4 z = B::mma16(is, sees, f32x4{0, 0, 0, 0});
-            settle(z);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) o[rt][j][r] = z[r] > 0.f ? NAN : o[rt][j][r];
-          }
-        }
-        wait_lds();
-#pragma unroll
-        for (int n = 0; n < kLoads; ++n) {
-          u32x4* at = (u32x4*)(vl + n * 1024 + l * 16);
-          u32x4 w = *at;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) w[e] &= ~((nan_bytes(w[e]) >> 7) * 0xffu);
-          *at = w;
-        }
-        wait_lds();
+        nan_from = min(nan_from, c0 + t);
+        nan_to = c0 + t + kSplitStep;
       }
+      wait_lds();
     }
     u32x2 w[OJ];
 #pragma unroll
@@ -501,7 +503,7 @@ __global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
   // The scales follow the first codes: both are on their way at once.
   for (int i = tid; i < ((cn + kSplitStep - 1) & -kSplitStep); i += kThreads) {
     const int blk = ((const int*)ks)[i];
-    ks[i] = blk < 0 ? 0.f : sk[blk * q.c_blk] * a.scale2;
+    ks[i] = blk < 0 ? NAN : sk[blk * q.c_blk] * a.scale2;
     vs[i] = sk[max(blk, 0) * q.c_blk + q.c_slab];
   }
   lds_barrier();
@@ -511,6 +513,11 @@ __global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
   __syncthreads();  // the tables are done with
   float* sums = (float*)lds;                      // [wave][16][DP]
   float* mls = sums + 4 * 16 * DP;                // [wave][RT * 16][2]
+  int* nans = (int*)(mls + 4 * RT * 16 * 2);      // [wave][2]
+  if (l == 0) {
+    nans[wave * 2] = nan_from;
+    nans[wave * 2 + 1] = nan_to;
+  }
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     sum[rt] += __shfl_xor(sum[rt], 16);
@@ -560,199 +567,277 @@ __global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
       }
     }
   }
+  nan_from = min(min(nans[0], nans[2]), min(nans[4], nans[6]));
+  nan_to = max(max(nans[1], nans[3]), max(nans[5], nans[7]));
+  if (nan_from < nan_to) {
+    wait_loads<0>();
+    __syncthreads();
+    spread_nan(a, sb, h, len, nq, seq.tok, nan_from, min(nan_to, c0 + cn), 0, rows,
+               direct ? nullptr : a.part + (int64_t)item * RT * 16 * DP, DP);
+  }
 }
 
 // ---------------------------------------------------------------------------
 // Many rows (prompt chunks): a workgroup takes 128 rows (queries and heads of a
-// group together, so that all share the head's tokens), 32 to a wave, and 64
-// tokens at a time: codes are converted once for the four waves and kept in LDS
-// as 16-bit rows, two tiles in turn.  32x32x16 products; values come out of LDS
-// transposed (ds_read_tr).
+// group together, so that all share the head's tokens), 32 to a wave, and 32
+// tokens at a time (a tile); 32x32x16 products.
+// Codes come to LDS four tiles ahead, as they are.  The lanes that asked for them
+// turn them into 16-bit rows, scale and all, for the four waves: keys two tiles
+// ahead, values one, read transposed (ds_read_tr).  A step holds its tile's
+// scores already: it turns them into probabilities while the matrix unit makes
+// the next tile's scores and the products with its values.
+// Places and scales of 256 tokens (a segment) stand in LDS; the next segment's are
+// brought in between: table entries, then scales, by the same kind of copy.
 // Bound by the matrix units, the exponentials and LDS.
 // ---------------------------------------------------------------------------
-constexpr int kTileTokens = 64;
+constexpr int kTile = 32, kSegment = 256, kPerSegment = kSegment / kTile, kAhead = 4;
+
+// As copy_to_lds, 4 bytes a lane: to lds + 4 * lane.
+__device__ __forceinline__ void copy_word_to_lds(const void* from, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off"
+               ::"v"(from), "s"(lds)
+               : "memory");
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)p;
+}
 
 __device__ __forceinline__ u32x2 read_tr(const uint8_t* p) {
   typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p));
 }
 
+// LDS: two tiles of keys and of values as 16-bit rows, the copied codes, two
+// segments' tables (place, key scale, value scale, position, table entry).
+template <int DP>
+struct TileLds {
+  static constexpr int kPitch = DP * 2 + 16, vPitch = DP * 2 + 32;  // bytes of a token's row
+  static constexpr int kBuf = kTile * kPitch, vBuf = kTile * vPitch, kRaw = 2 * kTile * DP;
+  static constexpr int kKeys = 0, kValues = 2 * kBuf, kCodes = kValues + 2 * vBuf;
+  static constexpr int kTables = kCodes + kAhead * kRaw, kTable = 5 * kSegment * 4;
+  static constexpr int kFlags = kTables + 2 * kTable;  // holes [2][4], NaN [4][2]
+  static constexpr int kBytes = kFlags + 16 * 4;
+};
+
 template <bool BF16, int DP>
-__global__ void __launch_bounds__(kThreads) attend_tile_kernel(AttendArgs a, int direct) {
+__global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1)
+    attend_tile_kernel(AttendArgs a, int direct) {
   using T = Ty<BF16>;
-  constexpr int KS = DP / 16, DB = DP / 32;
-  constexpr int kPitch = DP * 2 + 16, vPitch = DP * 2 + 32;  // bytes of a token's row in LDS
-  constexpr int kUnits = DP / 16;                            // 16 codes each
-  constexpr int UL = kTileTokens * kUnits / kThreads;        // units a thread loads (K, and V)
-  static_assert(UL >= 1, "");
-  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-  constexpr int kBuf = kTileTokens * (kPitch + vPitch);
-  float* const extra = (float*)(lds + 2 * kBuf);  // [2][64] positions, [2][64] mapped, [2][4] flags
+  using L = TileLds<DP>;
+  constexpr int KS = DP / 16, DB = DP / 32, CH = DP / 16;
+  constexpr int kPitch = L::kPitch, vPitch = L::vPitch;
+  constexpr int kUnits = kTile * CH;            // of 16 codes, of keys
+  constexpr int UT = 2 * kUnits / kThreads;     // units a thread brings, keys' first
+  extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+  int* const holes_of = (int*)(lds + L::kFlags);
+  int* const nans_of = holes_of + 8;
   const QLayout& q = a.q;
-  const int tid = threadIdx.x, wave = tid >> 6, l = tid & 63, c = l & 31, hf = l >> 5;
+  const int tid = threadIdx.x, l = tid & 63, c = l & 31, hf = l >> 5;
+  const int wave = scalar(tid >> 6);
 
   const int item = blockIdx.x;
   const Seq seq = seq_of(a, item);
   const int b = seq.b, sb = a.b0 + b, len = seq.len, nq = seq.nq, rows = nq * a.G;
-  const int nsplit = max(1, (len + a.chunk - 1) / a.chunk);
+  const int nsplit = max(1, scalar((len + a.chunk - 1) / a.chunk));
   const int tiles = (rows + kTileRows - 1) / kTileRows;
-  const int k = seq.k, h = k / (tiles * nsplit), kk = k - h * tiles * nsplit;
+  const int h = scalar(seq.k / (tiles * nsplit)), kk = seq.k - h * tiles * nsplit;
   // the last rows see the most tokens: they go first
-  const int tile = tiles - 1 - kk / nsplit, split = kk % nsplit;
+  const int tile = tiles - 1 - scalar(kk / nsplit), split = kk - (tiles - 1 - tile) * nsplit;
   const int r0 = tile * kTileRows, r = r0 + wave * 32 + c;
   const bool on = r < rows;
   const int i0 = r / a.G, head = h * a.G + (r - i0 * a.G);
   const int limit = on ? len - nq + i0 : -1;
-  const int all_see = len - nq + r0 / a.G;
-  const int last = len - nq + (min(rows, r0 + kTileRows) - 1) / a.G;  // the last slot seen
+  const int all_see = len - nq + scalar(r0 / a.G);
+  const int last = len - nq + scalar((min(rows, r0 + kTileRows) - 1) / a.G);  // last slot seen
   const int begin = split * a.chunk, end = min(min(begin + a.chunk, len), last + 1);
+  const int N = end > begin ? (end - begin + kTile - 1) / kTile : 0;
 
   const int64_t slab = 2 * (int64_t)a.layer;
   const uint8_t* kb = q.codes + slab * q.s_slab + sb * q.s_b + h * q.s_h;
-  const uint8_t* vb = kb + q.s_slab;
   const float* sk = q.scale + slab * q.c_slab + sb * q.c_b + h * q.c_h;
+  const int32_t* bt = q.bt ? q.bt + (int64_t)sb * q.max_blocks : nullptr;
   const int64_t slots = (((int64_t)a.layer * q.batch + sb) * q.heads + h) * (int64_t)q.cap;
 
   u32x4 qr[KS];
   {
     const uint16_t* src = (const uint16_t*)a.query +
                           (int64_t)(on ? seq.tok + i0 : 0) * a.q_token + (int64_t)head * a.q_head;
+    // The scores' factor counts as positive below: its sign goes to the queries.
+    const uint32_t flip = a.scale2 < 0.f ? 0x80008000u : 0u;
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       const int d = s * 16 + hf * 8;
       qr[s] = on && d < q.D ? *(const u32x4*)(src + d) : u32x4{0, 0, 0, 0};
+      qr[s] ^= flip;
     }
   }
+  // (A factor of 0 makes equal scores; as a tiny one it leaves hidden ones at -infinity.)
+  const float factor = fmaxf(fabsf(a.scale2), 0x1p-126f);
   float slope = 0.f, here = 0.f;
   if (a.slopes && limit >= 0) {
     slope = a.slopes[head] * kLog2e;
     here = (float)(q.position ? q.position[slots + limit] : limit);
   }
 
-  // Loading: unit u = tid + 256 i is 16 codes of token u / kUnits.
-  struct Codes {
-    u32x4 k[UL], v[UL];
-    float ks[UL], vs[UL], at;
-    int hole;
+  // ---- segments: thread tid stands for token begin + 256 g + tid ----
+  auto table = [&](int g, int which) {
+    return (float*)(lds + L::kTables + (g & 1) * L::kTable) + which * kSegment;
   };
-  auto block_of = [&](int (&blk)[UL], int t) {
-#pragma unroll
-    for (int i = 0; i < UL; ++i) {
-      const int tok = min(t + (tid + kThreads * i) / kUnits, len - 1), j = q.d_bs.div(tok);
-      blk[i] = q.bt ? q.bt[(int64_t)sb * q.max_blocks + j] : j;
-    }
-  };
-  auto load = [&](Codes& x, const int (&blk)[UL], int t) {
-    x.hole = 0;
-#pragma unroll
-    for (int i = 0; i < UL; ++i) {
-      const int u = tid + kThreads * i;
-      const int tok = min(t + u / kUnits, len - 1), j = q.d_bs.div(tok);
-      const bool hole = q.bt && (uint32_t)blk[i] >= (uint32_t)q.num_blocks;
-      const bool out = u % kUnits * 16 >= q.D;
-      const int64_t bk = hole ? 0 : blk[i];
-      const int64_t o = bk * q.s_blk + (int64_t)(tok - j * q.bs) * q.D + (out ? 0 : u % kUnits * 16);
-      x.k[i] = *(const u32x4*)(kb + o);
-      x.v[i] = *(const u32x4*)(vb + o);
-      x.ks[i] = sk[bk * q.c_blk];
-      x.vs[i] = sk[bk * q.c_blk + q.c_slab];
-      if (hole || out) x.k[i] = x.v[i] = u32x4{0, 0, 0, 0};
-      x.hole |= (int)hole << i;
-    }
-    if (a.slopes && tid < kTileTokens) {
-      const int tok = min(t + tid, len - 1);
-      x.at = (float)(q.position ? q.position[slots + tok] : tok);
-    }
-  };
-  auto store = [&](const Codes& x, int buf, bool mask) {
-    uint8_t* kl = lds + buf * kBuf;
-    uint8_t* vl = kl + kTileTokens * kPitch;
-    uint32_t odd = 0;
-#pragma unroll
-    for (int i = 0; i < UL; ++i) {
-      const int u = tid + kThreads * i, tok = u / kUnits, p = u % kUnits;
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        u32x4 y, z;
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          y[2 * w] = T::template cvt<false>(x.k[i][2 * e + w], x.ks[i]);
-          y[2 * w + 1] = T::template cvt<true>(x.k[i][2 * e + w], x.ks[i]);
-          z[2 * w] = T::template cvt<false>(x.v[i][2 * e + w], x.vs[i]);
-          z[2 * w + 1] = T::template cvt<true>(x.v[i][2 * e + w], x.vs[i]);
-        }
-        *(u32x4*)(kl + tok * kPitch + p * 32 + e * 16) = y;
-        *(u32x4*)(vl + tok * vPitch + p * 32 + e * 16) = z;
-      }
-      if (mask)
-#pragma unroll
-        for (int w = 0; w < 4; ++w) odd |= nan_bytes(x.v[i][w]);
-      if (p == 0) extra[128 + buf * 64 + tok] = (x.hole >> i) & 1 ? 0.f : 1.f;
-    }
-    const bool holes = __any(x.hole != 0), nans = __any(odd != 0);
-    if (l == 0) ((int*)extra)[256 + buf * 4 + wave] = (int)holes | (int)nans << 1;
-    if (a.slopes && tid < kTileTokens) extra[buf * 64 + tid] = x.at;
+  enum { kPlace, kKeyScale, kValueScale, kPosition, kEntry };
+  auto slot_of = [&](int g) { return min(begin + g * kSegment + tid, len - 1); };
+  // The table entry known: the place, and whether there is one.  Returns the block.
+  auto place = [&](int g, int entry) {
+    const int slot = slot_of(g), j = q.d_bs.div(slot);
+    int blk = bt ? entry : j;
+    const bool hole = bt && (uint32_t)blk >= (uint32_t)q.num_blocks;
+    blk = hole ? 0 : blk;
+    ((uint32_t*)table(g, kPlace))[tid] =
+        (uint32_t)(((int64_t)blk * q.s_blk + (int64_t)(slot - j * q.bs) * q.D) >> 4);
+    ((int*)table(g, kEntry))[tid] = hole ? -1 : 0;
+    const bool any = __any(hole);
+    if (l == 0) holes_of[(g & 1) * 4 + wave] = any;
+    if (a.slopes && !q.position) table(g, kPosition)[tid] = (float)slot;
+    return blk;
   };
 
-  f32x16 o[DB];
+  // ---- codes: unit u = tid + 256 i, the keys' kUnits first ----
+  const uint32_t raw = scalar(lds_address(lds + L::kCodes));
+  auto half_of = [&](int i) { return (wave * 64 + kThreads * i) / kUnits; };  // 1: values
+  auto fetch = [&](int n) {
+    const uint32_t* row = (const uint32_t*)table(n / kPerSegment, kPlace) + n % kPerSegment * kTile;
+    uint32_t at[UT];
+#pragma unroll
+    for (int i = 0; i < UT; ++i) {
+      const int u = (tid + kThreads * i) % kUnits, p = u % CH;
+      at[i] = row[u / CH] + (p * 16 < q.D ? p : 0);
+    }
+    wait_lds();
+#pragma unroll
+    for (int i = 0; i < UT; ++i)
+      copy_to_lds<false>(kb + half_of(i) * q.s_slab + (uint64_t)at[i] * 16,
+                         raw + (n & (kAhead - 1)) * L::kRaw + (wave * 64 + kThreads * i) * 16);
+  };
+  auto any_hole = [&](int g) {
+    const int* f = holes_of + (g & 1) * 4;
+    return bt && scalar(f[0] | f[1] | f[2] | f[3]);
+  };
+  int nan_from = INT32_MAX, nan_to = 0;  // tiles
+  // The keys (half 0) or values of tile n from codes to rows.
+  auto convert = [&](int n, int half) {
+    const float* scales = table(n / kPerSegment, kKeyScale + half) + n % kPerSegment * kTile;
+    const int* entry = (const int*)table(n / kPerSegment, kEntry) + n % kPerSegment * kTile;
+    uint8_t* to = lds + (half ? L::kValues + (n & 1) * L::vBuf : L::kKeys + (n & 1) * L::kBuf);
+    const int pitch = half ? vPitch : kPitch;
+    // Values that some row does not see: NaN becomes 0 (spread_nan).
+    const bool hidden = half && (begin + (n + 1) * kTile - 1 > all_see || any_hole(n / kPerSegment));
+#pragma unroll
+    for (int i = 0; i < UT; ++i) {
+      if (half_of(i) != half) continue;
+      const int u = (tid + kThreads * i) % kUnits, tok = u / CH, p = u % CH;
+      u32x4 x = *(const u32x4*)(lds + L::kCodes + (n & (kAhead - 1)) * L::kRaw +
+                                (tid + kThreads * i) * 16);
+      if ((bt && entry[tok] < 0) || p * 16 >= q.D) x = u32x4{0, 0, 0, 0};  // not there
+      const float scale = scales[tok];
+      if (hidden) {
+        uint32_t nan = 0;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const uint32_t y = nan_bytes(x[w]);
+          nan |= y;
+          x[w] &= ~((y >> 7) * 0xffu);
+        }
+        if (__any(nan != 0)) {
+          nan_from = min(nan_from, n);
+          nan_to = n + 1;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        *(u32x4*)(to + tok * pitch + p * 32 + e * 16) =
+            u32x4{T::template cvt<false>(x[2 * e], scale), T::template cvt<true>(x[2 * e], scale),
+                  T::template cvt<false>(x[2 * e + 1], scale),
+                  T::template cvt<true>(x[2 * e + 1], scale)};
+    }
+  };
+
+  f32x16 o[DB], s;
 #pragma unroll
   for (int d = 0; d < DB; ++d)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
   float m = kLow, sum = 0.f;
+  auto scores = [&](f32x16& z, int n, int e) {
+    const u32x4 y = *(const u32x4*)(lds + L::kKeys + (n & 1) * L::kBuf + c * kPitch + e * 32 +
+                                    hf * 16);
+    z = T::mma32(y, qr[e], z);
+  };
 
-  Codes x;
-  int blk[UL];
-  if (begin < end) {
-    block_of(blk, begin);
-    load(x, blk, begin);
-    block_of(blk, begin + kTileTokens);
-    store(x, 0, begin + kTileTokens - 1 > all_see);
+  if (N > 0) {
+    const int slot = slot_of(0), blk = place(0, bt ? bt[q.d_bs.div(slot)] : 0);
+    table(0, kKeyScale)[tid] = sk[blk * q.c_blk];
+    table(0, kValueScale)[tid] = sk[blk * q.c_blk + q.c_slab];
+    if (a.slopes && q.position) ((int*)table(0, kPosition))[tid] = q.position[slots + slot];
+    __syncthreads();
+    for (int n = 0; n < min(N, kAhead); ++n) fetch(n);
+    wait_loads<0>();
+    convert(0, 0);
+    convert(0, 1);
+    if (N > 1) convert(1, 0);
+    __syncthreads();
   }
-  __syncthreads();
-  int buf = 0;
-  for (int t = begin; t < end; t += kTileTokens, buf ^= 1) {
-    const bool more = t + kTileTokens < end;
-    if (more) {
-      load(x, blk, t + kTileTokens);
-      block_of(blk, t + 2 * kTileTokens);
-    }
-    const uint8_t* kl = lds + buf * kBuf;
-    const uint8_t* vl = kl + kTileTokens * kPitch;
-    const int* fl = (const int*)extra + 256 + buf * 4;
-    const int flags = __builtin_amdgcn_readfirstlane(fl[0] | fl[1] | fl[2] | fl[3]);
-    const bool mask = t + kTileTokens - 1 > all_see || (flags & 1);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+  for (int e = 0; e < KS; ++e) scores(s, 0, e);
+  settle(s);
 
-    f32x16 s[2];
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[u][i] = 0.f;
-#pragma unroll
-      for (int e = 0; e < KS; ++e) {
-        const u32x4 y = *(const u32x4*)(kl + (u * 32 + c) * kPitch + e * 32 + hf * 16);
-        s[u] = T::mma32(y, qr[e], s[u]);
+  for (int n = 0; n < N; ++n) {
+    const int t = begin + n * kTile, g = n / kPerSegment;
+    // The next segment's tables, before this tile's codes: each is there when the
+    // waits below have let what was asked for two steps ago arrive.
+    if ((g + 1) * kPerSegment < N) {
+      if (n % kPerSegment == 0 && bt)
+        copy_word_to_lds(bt + q.d_bs.div(slot_of(g + 1)),
+                         scalar(lds_address(table(g + 1, kEntry) + wave * 64)));
+      if (n % kPerSegment == 2) {
+        const int blk = place(g + 1, bt ? ((const int*)table(g + 1, kEntry))[tid] : 0);
+        const float* from = sk + blk * q.c_blk;
+        copy_word_to_lds(from, scalar(lds_address(table(g + 1, kKeyScale) + wave * 64)));
+        copy_word_to_lds(from + q.c_slab,
+                         scalar(lds_address(table(g + 1, kValueScale) + wave * 64)));
+        if (a.slopes && q.position)
+          copy_word_to_lds(q.position + slots + slot_of(g + 1),
+                           scalar(lds_address(table(g + 1, kPosition) + wave * 64)));
       }
     }
-    settle(s[0]);
-    settle(s[1]);
-    uint32_t seen = 0;  // bit u * 16 + i: token t + 32 u + (i / 4) * 8 + hf * 4 + i % 4
-    float most = -INFINITY;
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
+    if (n + kAhead < N) fetch(n + kAhead);
+
+    // This tile's scores: bias, what is hidden, the reference.
+    float mul = factor;
+    if (a.slopes) {
+      mul = 1.f;
+      const float* at = table(g, kPosition) + n % kPerSegment * kTile + hf * 4;
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        s[u][i] *= a.scale2;
-        const int at = u * 32 + (i / 4) * 8 + hf * 4 + i % 4;
-        if (a.slopes) s[u][i] += slope * (extra[buf * 64 + at] - here);
-        if (mask) {
-          const bool sees = t + at <= limit && extra[128 + buf * 64 + at] != 0.f;
-          s[u][i] = sees ? s[u][i] : -INFINITY;
-          seen |= (uint32_t)sees << (u * 16 + i);
-        }
-        most = fmaxf(most, s[u][i]);
+        const float x = at[(i / 4) * 8 + i % 4];
+        s[i] = s[i] * factor + slope * ((q.position ? (float)__float_as_int(x) : x) - here);
       }
     }
+    const bool holes = any_hole(g);
+    const bool mask = holes || t + kTile - 1 > all_see;
+    if (mask) {
+      const int* entry = (const int*)table(g, kEntry) + n % kPerSegment * kTile + hf * 4;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int at = (i / 4) * 8 + i % 4;
+        const bool sees = t + at + hf * 4 <= limit && !(holes && entry[at] < 0);
+        s[i] = sees ? s[i] : -INFINITY;
+      }
+    }
+    float most = s[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) most = fmaxf(most, s[i]);
+    most *= mul;
     if (__any(most > m + (kSlack + T::kLift))) {
       float up = fmaxf(most - T::kLift, m);
       up = fmaxf(up, __shfl_xor(up, 32));
@@ -762,81 +847,92 @@ __global__ void __launch_bounds__(kThreads) attend_tile_kernel(AttendArgs a, int
 #pragma unroll
       for (int d = 0; d < DB; ++d) o[d] = o[d] * f;
     }
+    const uint8_t* vt = lds + L::kValues + (n & 1) * L::vBuf + (hf * 4 + ((l & 15) >> 2)) * vPitch + ((l >> 4) & 1) * 32 +
+                        (l & 3) * 8;
+    f32x16 z;
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int i = 0; i < 16; ++i) z[i] = 0.f;
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {  // 16 tokens: slots hf * 8 + 0..7 of the inner axis
-        u32x4 p;
+    for (int e = 0; e < 2; ++e) {  // 16 tokens: slots hf * 8 + 0..7 of the inner axis
+      u32x4 p;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float p0 = exp2_(s[u][e * 8 + 2 * i] - m), p1 = exp2_(s[u][e * 8 + 2 * i + 1] - m);
-          sum += p0 + p1;
-          p[i] = T::pack(p0, p1);
-        }
-        const uint8_t* row = vl + (u * 32 + e * 16 + hf * 4 + ((l & 15) >> 2)) * vPitch +
-                             ((l >> 4) & 1) * 32 + (l & 3) * 8;
-#pragma unroll
-        for (int d = 0; d < DB; ++d) {
-          const u32x2 v0 = read_tr(row + d * 64), v1 = read_tr(row + 8 * vPitch + d * 64);
-          u32x4 v = {v0[0], v0[1], v1[0], v1[1]};
-          if (mask && (flags & 2)) {  // as in the kernel above
-            u32x4 is, sees;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const bool n0 = (v[i] & 0x7fff) > T::kInf, n1 = ((v[i] >> 16) & 0x7fff) > T::kInf;
-              is[i] = (n0 ? T::kOne : 0) | (n1 ? T::kOne << 16 : 0);
-              v[i] &= (n0 ? 0 : 0xffffu) | (n1 ? 0 : 0xffff0000u);
-              const int bit = u * 16 + e * 8 + 2 * i;
-              sees[i] = ((seen >> bit) & 1) * T::kOne | ((seen >> (bit + 1)) & 1) * (T::kOne << 16);
-            }
-            f32x16 z;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) z[i] = 0.f;
-            z = T::mma32(is, sees, z);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[d][i] = z[i] > 0.f ? NAN : o[d][i];
-          }
-          o[d] = T::mma32(v, p, o[d]);
-        }
+      for (int i = 0; i < 4; ++i) {
+        const float p0 = exp2_(s[e * 8 + 2 * i] * mul - m);
+        const float p1 = exp2_(s[e * 8 + 2 * i + 1] * mul - m);
+        sum += p0 + p1;
+        p[i] = T::pack(p0, p1);
       }
-    if (more) store(x, buf ^ 1, t + 2 * kTileTokens - 1 > all_see);
-    __syncthreads();
+#pragma unroll
+      for (int x = 0; x < KS / 2; ++x) scores(z, n + 1, e * (KS / 2) + x);
+#pragma unroll
+      for (int d = 0; d < DB; ++d) {
+        const u32x2 v0 = read_tr(vt + e * 16 * vPitch + d * 64);
+        const u32x2 v1 = read_tr(vt + (e * 16 + 8) * vPitch + d * 64);
+        o[d] = T::mma32(u32x4{v0[0], v0[1], v1[0], v1[1]}, p, o[d]);
+      }
+      // (else all of the step's LDS reads come first, and registers run out)
+      if (DP > 64) __builtin_amdgcn_sched_barrier(0);
+    }
+    settle(z);
+    s = z;
+    // What was asked for up to two steps ago is there: the keys of tile n + 2.
+    if (n + kAhead < N)
+      wait_loads<2 * UT>();
+    else
+      wait_loads<0>();
+    if (n + 2 < N) convert(n + 2, 0);
+    if (n + 1 < N) convert(n + 1, 1);
+    lds_barrier();
   }
 
   sum += __shfl_xor(sum, 32);
-  if (!on) return;
-  if (!direct) {
-    const int64_t at = (int64_t)item * kTileRows + wave * 32 + c;
+  if (l == 0) {
+    nans_of[wave * 2] = nan_from;
+    nans_of[wave * 2 + 1] = nan_to;
+  }
+  const int64_t at = (int64_t)item * kTileRows + wave * 32 + c;
+  if (on && !direct) {
     if (hf == 0) {
       a.ml[at * 2] = m;
       a.ml[at * 2 + 1] = sum;
     }
-    if (begin >= end) return;
+    if (N > 0) {
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+          *(f32x4*)(a.part + at * DP + d * 32 + (i / 4) * 8 + hf * 4) =
+              f32x4{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
+    }
+  }
+  if (on && direct) {
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    uint16_t* out = (uint16_t*)a.out + (int64_t)(seq.tok + i0) * a.o_token +
+                    (int64_t)head * a.o_head;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
-      for (int i = 0; i < 16; i += 4)
-        *(f32x4*)(a.part + at * DP + d * 32 + (i / 4) * 8 + hf * 4) =
-            f32x4{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
-    return;
-  }
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  uint16_t* out = (uint16_t*)a.out + (int64_t)(seq.tok + i0) * a.o_token + (int64_t)head * a.o_head;
-#pragma unroll
-  for (int d = 0; d < DB; ++d)
-#pragma unroll
-    for (int i = 0; i < 16; i += 4) {
-      const int at = d * 32 + (i / 4) * 8 + hf * 4;
-      if (at < q.D)
-        *(u32x2*)(out + at) = u32x2{T::pack(o[d][i] * inv, o[d][i + 1] * inv),
-                                    T::pack(o[d][i + 2] * inv, o[d][i + 3] * inv)};
+      for (int i = 0; i < 16; i += 4) {
+        const int x = d * 32 + (i / 4) * 8 + hf * 4;
+        if (x < q.D)
+          *(u32x2*)(out + x) = u32x2{T::pack(o[d][i] * inv, o[d][i + 1] * inv),
+                                     T::pack(o[d][i + 2] * inv, o[d][i + 3] * inv)};
+      }
+    if (hf == 0) {
+      const float lse2 = m + __log2f(sum);
+      const int64_t row = (int64_t)(seq.tok + i0) * a.q_heads + head;
+      if (a.lse) a.lse[(int64_t)a.row0 * a.q_heads + row] = sum == 0.f ? -INFINITY : lse2 * kLn2;
+      if (a.weigh) a.row_lse[row] = sum == 0.f ? INFINITY : lse2;
     }
-  if (hf == 0) {
-    const float lse2 = m + __log2f(sum);
-    const int64_t row = (int64_t)(seq.tok + i0) * a.q_heads + head;
-    if (a.lse) a.lse[(int64_t)a.row0 * a.q_heads + row] = sum == 0.f ? -INFINITY : lse2 * kLn2;
-    if (a.weigh) a.row_lse[row] = sum == 0.f ? INFINITY : lse2;
   }
+  wait_loads<0>();
+  __syncthreads();
+  nan_from = min(min(nans_of[0], nans_of[2]), min(nans_of[4], nans_of[6]));
+  nan_to = max(max(nans_of[1], nans_of[3]), max(nans_of[5], nans_of[7]));
+  if (nan_from < nan_to)
+    spread_nan(a, sb, h, len, nq, seq.tok, begin + nan_from * kTile,
+               min(end, begin + nan_to * kTile), r0, min(kTileRows, rows - r0),
+               direct ? nullptr : a.part + (int64_t)item * kTileRows * DP, DP);
 }
 
 // ---------------------------------------------------------------------------
@@ -859,10 +955,10 @@ __global__ void __launch_bounds__(kThreads) attend_join_kernel(AttendArgs a, int
   const int item = blockIdx.x;
   const Seq seq = seq_of(a, item);
   const int b = seq.b, sb = a.b0 + b, len = seq.len, nq = seq.nq, rows = nq * a.G;
-  const int nsplit = max(1, (len + a.chunk - 1) / a.chunk);
-  const int tiles = (rows + R - 1) / R;
-  const int h = seq.k / (tiles * nsplit), kk = seq.k - h * tiles * nsplit;
-  const int tile = tiles - 1 - kk / nsplit, split = kk % nsplit;
+  const int nsplit = max(1, scalar((len + a.chunk - 1) / a.chunk));
+  const int tiles = scalar((rows + R - 1) / R);
+  const int h = scalar(seq.k / (tiles * nsplit)), kk = seq.k - h * tiles * nsplit;
+  const int tile = tiles - 1 - scalar(kk / nsplit), split = kk - (tiles - 1 - tile) * nsplit;
   const int r0 = tile * R, nr = min(R, rows - r0);
   const float2* ml = (const float2*)a.ml + ((int64_t)item - split) * R;
 
@@ -973,12 +1069,13 @@ __global__ void __launch_bounds__(kThreads) attend_weigh_kernel(AttendArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t ql[2][32 * kPitch];
   __shared__ float lse[2][32], slopes[2][32], heres[2][32];
   const QLayout& q = a.q;
-  const int tid = threadIdx.x, wave = tid >> 6, l = tid & 63, c = l & 31, hf = l >> 5;
+  const int tid = threadIdx.x, l = tid & 63, c = l & 31, hf = l >> 5;
+  const int wave = scalar(tid >> 6);
   const int item = blockIdx.x;
   const Seq seq = seq_of(a, item);
   const int b = seq.b, sb = a.b0 + b, len = seq.len, nq = seq.nq, rows = nq * a.G;
   const int tiles = (len + kWeighTokens - 1) / kWeighTokens;
-  const int k = seq.k, h = k / tiles, t0 = (k - h * tiles) * kWeighTokens;
+  const int k = seq.k, h = scalar(k / tiles), t0 = (k - h * tiles) * kWeighTokens;
   const int tw = t0 + wave * 32;  // this wave's tokens
 
   const int64_t slab = 2 * (int64_t)a.layer;
@@ -1140,7 +1237,10 @@ hipError_t launch_attend_split(const AttendArgs& a, int rt, bool direct, hipStre
 
 hipError_t launch_attend_tile(const AttendArgs& a, bool direct, hipStream_t s) {
   const void* fn = pick(a, [](auto k) { return decltype(k)::tile(); });
-  const size_t lds = (size_t)2 * kTileTokens * (padded(a.q.D) * 4 + 48) + 264 * 4;
+  const int dp = padded(a.q.D);
+  const size_t lds = dp == 64    ? TileLds<64>::kBytes
+                     : dp == 128 ? TileLds<128>::kBytes
+                                 : TileLds<256>::kBytes;
   return launch(fn, dim3(a.items), lds, s, a, (int)direct);
 }
 

@@ -107,7 +107,7 @@ constexpr int split_waves(int DP, int RT) {
 inline size_t split_lds(int DP, int rt, int chunk, bool slopes) {
   const size_t tables = (size_t)4 * 2 * kSplitStep * DP + split_queries(DP, rt) +
                         (size_t)chunk * (slopes ? 16 : 12) + rt * 256 + 16;
-  const size_t join = (size_t)4 * 16 * DP * 4 + (size_t)4 * rt * 16 * 8;
+  const size_t join = (size_t)4 * 16 * DP * 4 + (size_t)4 * rt * 16 * 8 + 32;
   return tables > join ? tables : join;
 }
 inline int split_groups(int DP, int rt, int chunk, bool slopes) {
