@@ -722,42 +722,47 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1)
     return bt && scalar(f[0] | f[1] | f[2] | f[3]);
   };
   int nan_from = INT32_MAX, nan_to = 0;  // tiles
-  // The keys (half 0) or values of tile n from codes to rows.
-  auto convert = [&](int n, int half) {
-    const float* scales = table(n / kPerSegment, kKeyScale + half) + n % kPerSegment * kTile;
-    const int* entry = (const int*)table(n / kPerSegment, kEntry) + n % kPerSegment * kTile;
-    uint8_t* to = lds + (half ? L::kValues + (n & 1) * L::vBuf : L::kKeys + (n & 1) * L::kBuf);
-    const int pitch = half ? vPitch : kPitch;
+  // From codes to rows, unit i: of the keys of tile n + 2 or the values of tile n + 1.
+  struct Raw {
+    u32x4 x;
+    float scale;
+    int entry;
+  };
+  auto tile_of = [&](int i, int n) { return half_of(i) ? n + 1 : n + 2; };
+  auto take = [&](int i, int n) {
+    Raw y;
+    const int tok = n % kPerSegment * kTile + (tid + kThreads * i) % kUnits / CH;
+    y.x = *(const u32x4*)(lds + L::kCodes + (n & (kAhead - 1)) * L::kRaw +
+                          (tid + kThreads * i) * 16);
+    y.scale = table(n / kPerSegment, kKeyScale + half_of(i))[tok];
+    y.entry = bt ? ((const int*)table(n / kPerSegment, kEntry))[tok] : 0;
+    return y;
+  };
+  auto put = [&](Raw y, int i, int n) {
+    const int half = half_of(i), u = (tid + kThreads * i) % kUnits, tok = u / CH, p = u % CH;
+    uint8_t* to = lds + (half ? L::kValues + (n & 1) * L::vBuf : L::kKeys + (n & 1) * L::kBuf) +
+                  tok * (half ? vPitch : kPitch) + p * 32;
+    if (y.entry < 0 || p * 16 >= q.D) y.x = u32x4{0, 0, 0, 0};  // not there
     // Values that some row does not see: NaN becomes 0 (spread_nan).
-    const bool hidden = half && (begin + (n + 1) * kTile - 1 > all_see || any_hole(n / kPerSegment));
+    if (half && (begin + (n + 1) * kTile - 1 > all_see || any_hole(n / kPerSegment))) {
+      uint32_t nan = 0;
 #pragma unroll
-    for (int i = 0; i < UT; ++i) {
-      if (half_of(i) != half) continue;
-      const int u = (tid + kThreads * i) % kUnits, tok = u / CH, p = u % CH;
-      u32x4 x = *(const u32x4*)(lds + L::kCodes + (n & (kAhead - 1)) * L::kRaw +
-                                (tid + kThreads * i) * 16);
-      if ((bt && entry[tok] < 0) || p * 16 >= q.D) x = u32x4{0, 0, 0, 0};  // not there
-      const float scale = scales[tok];
-      if (hidden) {
-        uint32_t nan = 0;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const uint32_t y = nan_bytes(x[w]);
-          nan |= y;
-          x[w] &= ~((y >> 7) * 0xffu);
-        }
-        if (__any(nan != 0)) {
-          nan_from = min(nan_from, n);
-          nan_to = n + 1;
-        }
+      for (int w = 0; w < 4; ++w) {
+        const uint32_t z = nan_bytes(y.x[w]);
+        nan |= z;
+        y.x[w] &= ~((z >> 7) * 0xffu);
       }
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-        *(u32x4*)(to + tok * pitch + p * 32 + e * 16) =
-            u32x4{T::template cvt<false>(x[2 * e], scale), T::template cvt<true>(x[2 * e], scale),
-                  T::template cvt<false>(x[2 * e + 1], scale),
-                  T::template cvt<true>(x[2 * e + 1], scale)};
+      if (__any(nan != 0)) {
+        nan_from = min(nan_from, n);
+        nan_to = n + 1;
+      }
     }
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      *(u32x4*)(to + e * 16) = u32x4{
+          T::template cvt<false>(y.x[2 * e], y.scale), T::template cvt<true>(y.x[2 * e], y.scale),
+          T::template cvt<false>(y.x[2 * e + 1], y.scale),
+          T::template cvt<true>(y.x[2 * e + 1], y.scale)};
   };
 
   f32x16 o[DB], s;
@@ -766,10 +771,8 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
   float m = kLow, sum = 0.f;
-  auto scores = [&](f32x16& z, int n, int e) {
-    const u32x4 y = *(const u32x4*)(lds + L::kKeys + (n & 1) * L::kBuf + c * kPitch + e * 32 +
-                                    hf * 16);
-    z = T::mma32(y, qr[e], z);
+  auto key = [&](int n, int e) {
+    return *(const u32x4*)(lds + L::kKeys + (n & 1) * L::kBuf + c * kPitch + e * 32 + hf * 16);
   };
 
   if (N > 0) {
@@ -780,15 +783,17 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1)
     __syncthreads();
     for (int n = 0; n < min(N, kAhead); ++n) fetch(n);
     wait_loads<0>();
-    convert(0, 0);
-    convert(0, 1);
-    if (N > 1) convert(1, 0);
+#pragma unroll
+    for (int i = 0; i < UT; ++i) {
+      put(take(i, 0), i, 0);
+      if (!half_of(i) && N > 1) put(take(i, 1), i, 1);
+    }
     __syncthreads();
   }
 #pragma unroll
   for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
-  for (int e = 0; e < KS; ++e) scores(s, 0, e);
+  for (int e = 0; e < KS; ++e) s = T::mma32(key(0, e), qr[e], s);
   settle(s);
 
   for (int n = 0; n < N; ++n) {
@@ -811,6 +816,9 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1)
       }
     }
     if (n + kAhead < N) fetch(n + kAhead);
+    u32x4 y[KS];
+#pragma unroll
+    for (int e = 0; e < KS; ++e) y[e] = key(n + 1, e);
 
     // This tile's scores: bias, what is hidden, the reference.
     float mul = factor;
@@ -849,39 +857,52 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1)
     }
     const uint8_t* vt = lds + L::kValues + (n & 1) * L::vBuf + (hf * 4 + ((l & 15) >> 2)) * vPitch + ((l >> 4) & 1) * 32 +
                         (l & 3) * 8;
+    // Products with exponentials in between (the barriers keep them so): the next
+    // tile's scores, of which the last is out of range and used by nothing, ...
+    auto value = [&](int e, int d) {
+      const u32x2 v0 = read_tr(vt + e * 16 * vPitch + d * 64);
+      const u32x2 v1 = read_tr(vt + (e * 16 + 8) * vPitch + d * 64);
+      return u32x4{v0[0], v0[1], v1[0], v1[1]};
+    };
     f32x16 z;
+    u32x4 p[2], v[DB];  // p: 16 tokens each, slots hf * 8 + 0..7 of the inner axis
 #pragma unroll
     for (int i = 0; i < 16; ++i) z[i] = 0.f;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {  // 16 tokens: slots hf * 8 + 0..7 of the inner axis
-      u32x4 p;
+    for (int e = 0; e < KS; ++e) {
+      z = T::mma32(y[e], qr[e], z);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float p0 = exp2_(s[e * 8 + 2 * i] * mul - m);
-        const float p1 = exp2_(s[e * 8 + 2 * i + 1] * mul - m);
+      for (int i = e * 8 / KS; i < (e + 1) * 8 / KS; ++i) {
+        const float p0 = exp2_(s[2 * i] * mul - m), p1 = exp2_(s[2 * i + 1] * mul - m);
         sum += p0 + p1;
-        p[i] = T::pack(p0, p1);
+        p[i / 4][i % 4] = T::pack(p0, p1);
       }
-#pragma unroll
-      for (int x = 0; x < KS / 2; ++x) scores(z, n + 1, e * (KS / 2) + x);
-#pragma unroll
-      for (int d = 0; d < DB; ++d) {
-        const u32x2 v0 = read_tr(vt + e * 16 * vPitch + d * 64);
-        const u32x2 v1 = read_tr(vt + (e * 16 + 8) * vPitch + d * 64);
-        o[d] = T::mma32(u32x4{v0[0], v0[1], v1[0], v1[1]}, p, o[d]);
-      }
-      // (else all of the step's LDS reads come first, and registers run out)
-      if (DP > 64) __builtin_amdgcn_sched_barrier(0);
+      if (e >= DB) v[e - DB] = value(0, e - DB);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    settle(z);
-    s = z;
-    // What was asked for up to two steps ago is there: the keys of tile n + 2.
+    // ... and the products with the values, the codes' conversion in between.  What
+    // was asked for up to two steps ago is there: the keys of tile n + 2.
     if (n + kAhead < N)
       wait_loads<2 * UT>();
     else
       wait_loads<0>();
-    if (n + 2 < N) convert(n + 2, 0);
-    if (n + 1 < N) convert(n + 1, 1);
+    Raw raws[UT];
+#pragma unroll
+    for (int i = 0; i < UT; ++i)
+      if (tile_of(i, n) < N) raws[i] = take(i, tile_of(i, n));
+#pragma unroll
+    for (int d = 0; d < DB; ++d) {
+      o[d] = T::mma32(v[d], p[0], o[d]);
+      v[d] = value(1, d);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < UT; ++i)
+      if (tile_of(i, n) < N) put(raws[i], i, tile_of(i, n));
+#pragma unroll
+    for (int d = 0; d < DB; ++d) o[d] = T::mma32(v[d], p[1], o[d]);
+    settle(z);
+    s = z;
     lds_barrier();
   }
 
