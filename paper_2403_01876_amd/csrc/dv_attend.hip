@@ -702,7 +702,14 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1)
 
   // ---- codes: unit u = tid + 256 i, the keys' kUnits first ----
   const uint32_t raw = scalar(lds_address(lds + L::kCodes));
-  auto half_of = [&](int i) { return (wave * 64 + kThreads * i) / kUnits; };  // 1: values
+  // 0: keys, 1: values
+  auto half_of = [&](int i) {
+    if constexpr (kUnits >= kThreads)
+      return i / (kUnits / kThreads);
+    else
+      return wave * 64 / kUnits;
+  };
+  const uint8_t* const vb = kb + q.s_slab;
   auto fetch = [&](int n) {
     const uint32_t* row = (const uint32_t*)table(n / kPerSegment, kPlace) + n % kPerSegment * kTile;
     uint32_t at[UT];
@@ -714,7 +721,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1)
     wait_lds();
 #pragma unroll
     for (int i = 0; i < UT; ++i)
-      copy_to_lds<false>(kb + half_of(i) * q.s_slab + (uint64_t)at[i] * 16,
+      copy_to_lds<false>((half_of(i) ? vb : kb) + (uint64_t)at[i] * 16,
                          raw + (n & (kAhead - 1)) * L::kRaw + (wave * 64 + kThreads * i) * 16);
   };
   auto any_hole = [&](int g) {
@@ -722,6 +729,9 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1)
     return bt && scalar(f[0] | f[1] | f[2] | f[3]);
   };
   int nan_from = INT32_MAX, nan_to = 0;  // tiles
+  // Whether this segment, and the next, have unmapped slots.
+  bool holes = false, next_holes = false;
+  auto holes_at = [&](int n, int now) { return n / kPerSegment == now / kPerSegment ? holes : next_holes; };
   // From codes to rows, unit i: of the keys of tile n + 2 or the values of tile n + 1.
   struct Raw {
     u32x4 x;
@@ -729,22 +739,22 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1)
     int entry;
   };
   auto tile_of = [&](int i, int n) { return half_of(i) ? n + 1 : n + 2; };
-  auto take = [&](int i, int n) {
+  auto take = [&](int i, int n, bool holes) {
     Raw y;
     const int tok = n % kPerSegment * kTile + (tid + kThreads * i) % kUnits / CH;
     y.x = *(const u32x4*)(lds + L::kCodes + (n & (kAhead - 1)) * L::kRaw +
                           (tid + kThreads * i) * 16);
     y.scale = table(n / kPerSegment, kKeyScale + half_of(i))[tok];
-    y.entry = bt ? ((const int*)table(n / kPerSegment, kEntry))[tok] : 0;
+    y.entry = holes ? ((const int*)table(n / kPerSegment, kEntry))[tok] : 0;
     return y;
   };
-  auto put = [&](Raw y, int i, int n) {
+  auto put = [&](Raw y, int i, int n, bool holes) {
     const int half = half_of(i), u = (tid + kThreads * i) % kUnits, tok = u / CH, p = u % CH;
     uint8_t* to = lds + (half ? L::kValues + (n & 1) * L::vBuf : L::kKeys + (n & 1) * L::kBuf) +
                   tok * (half ? vPitch : kPitch) + p * 32;
     if (y.entry < 0 || p * 16 >= q.D) y.x = u32x4{0, 0, 0, 0};  // not there
     // Values that some row does not see: NaN becomes 0 (spread_nan).
-    if (half && (begin + (n + 1) * kTile - 1 > all_see || any_hole(n / kPerSegment))) {
+    if (half && (begin + (n + 1) * kTile - 1 > all_see || holes)) {
       uint32_t nan = 0;
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
@@ -781,12 +791,13 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1)
     table(0, kValueScale)[tid] = sk[blk * q.c_blk + q.c_slab];
     if (a.slopes && q.position) ((int*)table(0, kPosition))[tid] = q.position[slots + slot];
     __syncthreads();
+    holes = any_hole(0);
     for (int n = 0; n < min(N, kAhead); ++n) fetch(n);
     wait_loads<0>();
 #pragma unroll
     for (int i = 0; i < UT; ++i) {
-      put(take(i, 0), i, 0);
-      if (!half_of(i) && N > 1) put(take(i, 1), i, 1);
+      put(take(i, 0, holes), i, 0, holes);
+      if (!half_of(i) && N > 1) put(take(i, 1, holes), i, 1, holes);
     }
     __syncthreads();
   }
@@ -800,7 +811,9 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1)
     const int t = begin + n * kTile, g = n / kPerSegment;
     // The next segment's tables, before this tile's codes: each is there when the
     // waits below have let what was asked for two steps ago arrive.
+    if (n % kPerSegment == 0 && n > 0) holes = next_holes;
     if ((g + 1) * kPerSegment < N) {
+      if (n % kPerSegment == 4) next_holes = any_hole(g + 1);
       if (n % kPerSegment == 0 && bt)
         copy_word_to_lds(bt + q.d_bs.div(slot_of(g + 1)),
                          scalar(lds_address(table(g + 1, kEntry) + wave * 64)));
@@ -831,7 +844,6 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1)
         s[i] = s[i] * factor + slope * ((q.position ? (float)__float_as_int(x) : x) - here);
       }
     }
-    const bool holes = any_hole(g);
     const bool mask = holes || t + kTile - 1 > all_see;
     if (mask) {
       const int* entry = (const int*)table(g, kEntry) + n % kPerSegment * kTile + hf * 4;
@@ -889,7 +901,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1)
     Raw raws[UT];
 #pragma unroll
     for (int i = 0; i < UT; ++i)
-      if (tile_of(i, n) < N) raws[i] = take(i, tile_of(i, n));
+      if (tile_of(i, n) < N) raws[i] = take(i, tile_of(i, n), holes_at(tile_of(i, n), n));
 #pragma unroll
     for (int d = 0; d < DB; ++d) {
       o[d] = T::mma32(v[d], p[0], o[d]);
@@ -898,7 +910,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1)
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < UT; ++i)
-      if (tile_of(i, n) < N) put(raws[i], i, tile_of(i, n));
+      if (tile_of(i, n) < N) put(raws[i], i, tile_of(i, n), holes_at(tile_of(i, n), n));
 #pragma unroll
     for (int d = 0; d < DB; ++d) o[d] = T::mma32(v[d], p[1], o[d]);
     settle(z);
