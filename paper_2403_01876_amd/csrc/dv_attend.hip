@@ -710,8 +710,10 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1)
       return wave * 64 / kUnits;
   };
   const uint8_t* const vb = kb + q.s_slab;
-  auto fetch = [&](int n) {
-    const uint32_t* row = (const uint32_t*)table(n / kPerSegment, kPlace) + n % kPerSegment * kTile;
+  auto fetch = [&](int n, int last) {  // past the last tile: that one again
+    const int from = min(n, last);
+    const uint32_t* row =
+        (const uint32_t*)table(from / kPerSegment, kPlace) + from % kPerSegment * kTile;
     uint32_t at[UT];
 #pragma unroll
     for (int i = 0; i < UT; ++i) {
@@ -792,7 +794,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1)
     if (a.slopes && q.position) ((int*)table(0, kPosition))[tid] = q.position[slots + slot];
     __syncthreads();
     holes = any_hole(0);
-    for (int n = 0; n < min(N, kAhead); ++n) fetch(n);
+    for (int n = 0; n < kAhead; ++n) fetch(n, N - 1);
     wait_loads<0>();
 #pragma unroll
     for (int i = 0; i < UT; ++i) {
@@ -828,7 +830,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1)
                            scalar(lds_address(table(g + 1, kPosition) + wave * 64)));
       }
     }
-    if (n + kAhead < N) fetch(n + kAhead);
+    fetch(n + kAhead, N - 1);
     u32x4 y[KS];
 #pragma unroll
     for (int e = 0; e < KS; ++e) y[e] = key(n + 1, e);
@@ -888,20 +890,20 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1)
         const float p0 = exp2_(s[2 * i] * mul - m), p1 = exp2_(s[2 * i + 1] * mul - m);
         sum += p0 + p1;
         p[i / 4][i % 4] = T::pack(p0, p1);
+        asm volatile("" : "+v"(p[i / 4][i % 4]));  // here, not where it is first used
       }
       if (e >= DB) v[e - DB] = value(0, e - DB);
       __builtin_amdgcn_sched_barrier(0);
     }
     // ... and the products with the values, the codes' conversion in between.  What
     // was asked for up to two steps ago is there: the keys of tile n + 2.
-    if (n + kAhead < N)
-      wait_loads<2 * UT>();
-    else
-      wait_loads<0>();
+    // (Past the last tile too, where nothing reads what comes of it: no branch keeps
+    // products and exponentials apart.)
+    wait_loads<2 * UT>();
     Raw raws[UT];
 #pragma unroll
     for (int i = 0; i < UT; ++i)
-      if (tile_of(i, n) < N) raws[i] = take(i, tile_of(i, n), holes_at(tile_of(i, n), n));
+      raws[i] = take(i, tile_of(i, n), holes_at(tile_of(i, n), n));
 #pragma unroll
     for (int d = 0; d < DB; ++d) {
       o[d] = T::mma32(v[d], p[0], o[d]);
@@ -910,7 +912,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1)
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < UT; ++i)
-      if (tile_of(i, n) < N) put(raws[i], i, tile_of(i, n), holes_at(tile_of(i, n), n));
+      put(raws[i], i, tile_of(i, n), holes_at(tile_of(i, n), n));
 #pragma unroll
     for (int d = 0; d < DB; ++d) o[d] = T::mma32(v[d], p[1], o[d]);
     settle(z);
