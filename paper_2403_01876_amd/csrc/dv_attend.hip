@@ -1093,36 +1093,44 @@ __global__ void __launch_bounds__(kThreads) attend_join_kernel(AttendArgs a, int
 }
 
 // ---------------------------------------------------------------------------
-// Weights from many rows: a workgroup takes 128 tokens of a head, 32 to a wave,
-// and every row that may see them; p = exp2(s2 - lse2).  Each sum is one lane's
-// and the lanes' are added in a fixed order.  Bound as the product is.
+// Weights from many rows: a workgroup takes 128 tokens of a head and every row
+// that may see them; p = exp2(s2 - lse2).  A wave holds 64 tokens' keys and takes
+// every other 32 rows, which the workgroup copies to LDS two steps ahead (16-byte
+// pieces stored at piece ^ key(row), as above).  Each sum is one lane's; the
+// lanes', then the two waves', are added in a fixed order.
+// Bound by the exponentials and the product.
 // ---------------------------------------------------------------------------
 template <bool BF16, int DP>
-__global__ void __launch_bounds__(kThreads) attend_weigh_kernel(AttendArgs a) {
+__global__ void __launch_bounds__(kThreads, DP <= 128 ? 3 : 1) attend_weigh_kernel(AttendArgs a) {
   using T = Ty<BF16>;
-  constexpr int KS = DP / 16, kPitch = DP * 2 + 16, UL = 32 * DP * 2 / 16 / kThreads;
-  __shared__ __attribute__((aligned(16))) uint8_t ql[2][32 * kPitch];
-  __shared__ float lse[2][32], slopes[2][32], heres[2][32];
+  constexpr int KS = DP / 16, CH = DP / 8;       // products; 16-byte pieces of a row
+  constexpr int kStep = 64, kBytes = kStep * DP * 2, kRing = 3;
+  constexpr int kLoads = kBytes / 1024 / 4;      // copies of a wave
+  __shared__ __attribute__((aligned(1024))) uint8_t rows_of[kRing * kBytes];
+  __shared__ __attribute__((aligned(16))) float words[kRing][4][64];  // rows' lse, slope
+  __shared__ __attribute__((aligned(16))) float token_at[kWeighTokens];  // positions
+  __shared__ float part[2][64];
   const QLayout& q = a.q;
   const int tid = threadIdx.x, l = tid & 63, c = l & 31, hf = l >> 5;
-  const int wave = scalar(tid >> 6);
+  const int wave = scalar(tid >> 6), odd = wave >> 1;
   const int item = blockIdx.x;
   const Seq seq = seq_of(a, item);
   const int b = seq.b, sb = a.b0 + b, len = seq.len, nq = seq.nq, rows = nq * a.G;
   const int tiles = (len + kWeighTokens - 1) / kWeighTokens;
-  const int k = seq.k, h = scalar(k / tiles), t0 = (k - h * tiles) * kWeighTokens;
-  const int tw = t0 + wave * 32;  // this wave's tokens
+  const int h = scalar(seq.k / tiles), t0 = (seq.k - h * tiles) * kWeighTokens;
+  const int tw = t0 + (wave & 1) * 64;  // this wave's tokens
 
   const int64_t slab = 2 * (int64_t)a.layer;
   const int64_t slots = (((int64_t)a.layer * q.batch + sb) * q.heads + h) * (int64_t)q.cap;
-  u32x4 kr[KS];
-  uint32_t mapped;  // bit i: token tw + i
-  {
-    const int tok = min(tw + c, len - 1), j = q.d_bs.div(tok);
+  u32x4 kr[2][KS];
+  uint32_t mapped[2];  // bit i: token tw + 32 u + i
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int tok = min(tw + u * 32 + c, len - 1), j = q.d_bs.div(tok);
     int64_t blk = q.bt ? q.bt[(int64_t)sb * q.max_blocks + j] : j;
     const bool hole = q.bt && (uint64_t)blk >= (uint64_t)q.num_blocks;
     blk = hole ? 0 : blk;
-    mapped = (uint32_t)__ballot(!hole);
+    mapped[u] = (uint32_t)__ballot(!hole);
     const uint8_t* p = q.codes + slab * q.s_slab + sb * q.s_b + h * q.s_h + blk * q.s_blk +
                        (int64_t)(tok - j * q.bs) * q.D;
     const float scale = q.scale[slab * q.c_slab + sb * q.c_b + h * q.c_h + blk * q.c_blk];
@@ -1131,102 +1139,125 @@ __global__ void __launch_bounds__(kThreads) attend_weigh_kernel(AttendArgs a) {
       const int d = s * 16 + hf * 8;
       u32x2 w = {0, 0};
       if (d < q.D) w = *(const u32x2*)(p + d);
-      kr[s] = u32x4{T::template cvt<false>(w[0], scale), T::template cvt<true>(w[0], scale),
-                    T::template cvt<false>(w[1], scale), T::template cvt<true>(w[1], scale)};
+      kr[u][s] = u32x4{T::template cvt<false>(w[0], scale), T::template cvt<true>(w[0], scale),
+                       T::template cvt<false>(w[1], scale), T::template cvt<true>(w[1], scale)};
     }
   }
-  float at[16];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int tok = min(tw + (i / 4) * 8 + hf * 4 + i % 4, len - 1);
-    at[i] = a.slopes ? (float)(q.position ? q.position[slots + tok] : tok) : 0.f;
+  if (a.slopes && tid < kWeighTokens) {
+    const int x = min(t0 + tid, len - 1);
+    token_at[tid] = (float)(q.position ? q.position[slots + x] : x);
   }
 
   const int before = len - nq;  // query i sees slots up to before + i
-  u32x4 x[UL];
-  float x_lse = 0.f, x_slope = 0.f, x_here = 0.f;
-  auto load = [&](int r0) {
+  // the first row that sees the workgroup's first token
+  const int from = max(0, t0 - before) * a.G & -kStep;
+  const int steps = rows > from ? (rows - from + kStep - 1) / kStep : 0;
+  auto key_of = [](int row) { return CH == 8 ? (row >> 1) & 7 : row & 15; };
+  const uint32_t rows_at = scalar(lds_address(rows_of)), words_at = scalar(lds_address(words));
+  // (Rows past the last are the last again, and so are steps; both are hidden.)
+  auto fetch = [&](int k) {
+    const int r0 = from + min(k, steps - 1) * kStep, slot = k % kRing;
+    wait_lds();
 #pragma unroll
-    for (int i = 0; i < UL; ++i) {
-      const int u = tid + kThreads * i, r = r0 + u / (DP / 8), d = u % (DP / 8) * 8;
-      const int qi = r / a.G, head = h * a.G + (r - qi * a.G);
-      x[i] = u32x4{0, 0, 0, 0};
-      if (r < rows && d < q.D)
-        x[i] = *(const u32x4*)((const uint16_t*)a.query + (int64_t)(seq.tok + qi) * a.q_token +
-                               (int64_t)head * a.q_head + d);
+    for (int i = 0; i < kLoads; ++i) {
+      const int u = tid + kThreads * i, row = u / CH, r = min(r0 + row, rows - 1);
+      const int qi = a.d_G.div(r), head = h * a.G + (r - qi * a.G);
+      const int d = (u % CH ^ key_of(row)) * 8;
+      copy_to_lds<false>((const uint8_t*)((const uint16_t*)a.query +
+                                          (uint64_t)(uint32_t)(seq.tok + qi) * (uint32_t)a.q_token +
+                                          (uint64_t)(uint32_t)head * (uint32_t)a.q_head +
+                                          (d < q.D ? d : 0)),
+                         rows_at + slot * kBytes + (wave * 64 + kThreads * i) * 16);
     }
-    if (tid < 32) {
-      const int r = r0 + tid, qi = r / a.G, head = h * a.G + (r - qi * a.G);
-      x_lse = INFINITY;
-      x_slope = x_here = 0.f;
-      if (r < rows) {
-        x_lse = a.row_lse[(int64_t)(seq.tok + qi) * a.q_heads + head];
-        if (a.slopes && before + qi >= 0) {
-          x_slope = a.slopes[head] * kLog2e;
-          x_here = (float)(q.position ? q.position[slots + before + qi] : before + qi);
-        }
-      }
-    }
-  };
-  auto store = [&](int buf) {
-#pragma unroll
-    for (int i = 0; i < UL; ++i) {
-      const int u = tid + kThreads * i;
-      *(u32x4*)(ql[buf] + u / (DP / 8) * kPitch + u % (DP / 8) * 16) = x[i];
-    }
-    if (tid < 32) {
-      lse[buf][tid] = x_lse;
-      slopes[buf][tid] = x_slope;
-      heres[buf][tid] = x_here;
-    }
+    const int r = min(r0 + odd * 32 + c, rows - 1), qi = a.d_G.div(r), head = h * a.G + r - qi * a.G;
+    const float* word = a.row_lse + (int64_t)(seq.tok + qi) * a.q_heads + head;
+    if (a.slopes && hf) word = a.slopes + head;
+    copy_word_to_lds(word, words_at + (slot * 4 + wave) * 256);
   };
 
-  float sum[16];
+  float sum[2][16];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) sum[i] = 0.f;
-  // the first row that sees the workgroup's first token
-  const int from = max(0, t0 - before) * a.G & ~31;
-  int buf = 0;
-  if (from < rows) {
-    load(from);
-    store(0);
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum[u][i] = 0.f;
+  if (steps > 0) {
+    fetch(0);
+    fetch(1);
   }
-  __syncthreads();
-  for (int r0 = from; r0 < rows; r0 += 32, buf ^= 1) {
-    const bool more = r0 + 32 < rows;
-    if (more) load(r0 + 32);
-    f32x16 s;
+  for (int k = 0; k < steps; ++k) {
+    wait_loads<kLoads + 1>();  // all but the next step's
+    lds_barrier();
+    fetch(k + 2);
+    const int slot = k % kRing, r0 = from + k * kStep + odd * 32;
+    const uint8_t* ql = rows_of + slot * kBytes + (odd * 32 + c) * DP * 2;
+    const int kk = key_of(c);  // (32 rows on the key is the same)
+    f32x16 s[2];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = 0.f;
+    for (int i = 0; i < 16; ++i) s[0][i] = s[1][i] = 0.f;
 #pragma unroll
-    for (int e = 0; e < KS; ++e)
-      s = T::mma32(kr[e], *(const u32x4*)(ql[buf] + c * kPitch + e * 32 + hf * 16), s);
-    settle(s);
-    const float lse2 = lse[buf][c], sl = slopes[buf][c], here = heres[buf][c];
-    const int limit = before + (r0 + c) / a.G;
-    const bool mask = before + r0 / a.G < tw + 31 || mapped != 0xffffffffu;
+    for (int e = 0; e < KS; ++e) {
+      // (pieces past head_dim repeat the row's first: they meet zeros of the keys)
+      const u32x4 y = *(const u32x4*)(ql + (((2 * e + hf) ^ kk) << 4));
+      s[0] = T::mma32(kr[0][e], y, s[0]);
+      s[1] = T::mma32(kr[1][e], y, s[1]);
+    }
+    settle(s[0]);
+    settle(s[1]);
+    const float* w = words[slot][wave];
+    const float lse2 = w[c];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[u][i] = s[u][i] * a.scale2 - lse2;
+    const int limit = r0 + c < rows ? before + (int)a.d_G.div(r0 + c) : -1;
+    if (a.slopes) {
+      const float slope = w[32 + c] * kLog2e;
+      const float here = limit < 0 ? 0.f : q.position ? (float)q.position[slots + limit] : (float)limit;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          s[u][i] += slope * (token_at[tw - t0 + u * 32 + (i / 4) * 8 + hf * 4 + i % 4] - here);
+    }
+    // (lse is +infinity for a row that sees nothing: its p are 0, or NaN, and hidden)
+    if (before + scalar(r0 / a.G) < tw + 63 || r0 + 32 > rows ||
+        (mapped[0] & mapped[1]) != 0xffffffffu) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int o = (i / 4) * 8 + hf * 4 + i % 4;
+          const bool sees = tw + u * 32 + o <= limit && ((mapped[u] >> o) & 1) && lse2 != INFINITY;
+          s[u][i] = sees ? s[u][i] : -INFINITY;
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sum[u][i] += exp2_(s[u][i]);
+  }
+  wait_loads<0>();  // (nothing arrives after the workgroup's end)
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const int o = (i / 4) * 8 + hf * 4 + i % 4;
-      float y = s[i] * a.scale2;
-      if (a.slopes) y += sl * (at[i] - here);
-      float p = exp2_(y - lse2);
-      if (mask) p = tw + o <= limit && ((mapped >> o) & 1) && lse2 != INFINITY ? p : 0.f;
-      sum[i] += p;
-    }
-    if (more) store(buf ^ 1);
-    __syncthreads();
-  }
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-#pragma unroll
-    for (int x = 16; x; x >>= 1) sum[i] += __shfl_xor(sum[i], x);
-    const int tok = tw + (i / 4) * 8 + hf * 4 + i % 4;
-    if (c == i && tok < len) {
-      float* w = q.weight + slots + tok;
-      *w = a.decay == 0.f ? sum[i] : a.decay * *w + sum[i];
+      for (int x = 16; x; x >>= 1) sum[u][i] += __shfl_xor(sum[u][i], x);
+      if (odd && c == i) part[wave & 1][u * 32 + (i / 4) * 8 + hf * 4 + i % 4] = sum[u][i];
     }
-  }
+  __syncthreads();
+  if (odd) return;
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int o = u * 32 + (i / 4) * 8 + hf * 4 + i % 4;
+      if (c == i && tw + o < len) {
+        float* to = q.weight + slots + tw + o;
+        const float total = sum[u][i] + part[wave & 1][o];
+        *to = a.decay == 0.f ? total : a.decay * *to + total;
+      }
+    }
 }
 
 template <typename... More>

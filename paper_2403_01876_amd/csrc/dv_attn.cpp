@@ -268,7 +268,7 @@ int attend(const dv_quant* c, int32_t mb, int32_t layer, const int32_t* q_len,
   const int64_t D = v.D;
   const int64_t strides[4] = {u->q_token, u->q_head, u->out_token, u->out_head};
   for (int64_t s : strides)
-    if (s < 0 || s % 8 != 0 || s > (1ll << 40)) return DV_ERR_INVALID;
+    if (s < 0 || s % 8 != 0 || s >= (1ll << 31)) return DV_ERR_INVALID;
   if (!u->q || !u->out || !aligned16(u->q) || !aligned16(u->out) || !aligned4(u->slopes) ||
       !aligned4(u->lse) || !aligned16(u->workspace))
     return DV_ERR_INVALID;
@@ -314,6 +314,7 @@ int attend(const dv_quant* c, int32_t mb, int32_t layer, const int32_t* q_len,
   a.decay = u->decay;
   a.layer = layer;
   a.G = (int32_t)G;
+  a.d_G = dv::fast_div((uint32_t)G);
   a.q_heads = u->q_heads;
   a.chunk = p.chunk;
   a.weigh = u->weigh != 0;

@@ -80,6 +80,7 @@ struct AttendArgs {
   int32_t layer, b0, nseq, items;
   int32_t G, q_heads, chunk;  // chunk: tokens of a split (rows of a tile where there are many)
   int32_t weigh, bf16, row0;  // row0: rows of q before this launch's
+  FastDiv d_G;
   int32_t nt, pad;            // whether the codes are read past the caches
   int32_t item[kQSeqs];       // work items of earlier sequences; INT32_MAX past the last
   int32_t tok[kQSeqs + 1];    // queries of earlier sequences
