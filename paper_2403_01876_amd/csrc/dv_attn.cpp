@@ -501,6 +501,8 @@ int dv_evict(const dv_quant* src, int32_t src_mb, const dv_quant* dst, int32_t d
   a.in_place = in_place;
   a.most = (int32_t)longest;
   a.blocks = (int32_t)blocks;
+  // Blocks whose tokens are looked up together: 128 tokens, or a block a wave.
+  a.group = (int32_t)std::max<int64_t>(4, 128 / a.d.bs / 4 * 4);
   a.d_du = dv::fast_div((uint32_t)(v.D / 16));
   hipStream_t st = static_cast<hipStream_t>(stream);
   for (int32_t l = l0; l < l1; l += kLayers) {
@@ -510,10 +512,17 @@ int dv_evict(const dv_quant* src, int32_t src_mb, const dv_quant* dst, int32_t d
     for (int64_t b0 = 0; b0 < v.B; b0 += seqs) {
       a.b0 = (int32_t)b0;
       a.nseq = (int32_t)std::min<int64_t>(seqs, v.B - b0);
-      for (int i = 0; i < a.nseq; ++i) {
+      int64_t items = 0;
+      for (int i = 0; i < kQSeqs; ++i) {
+        a.item[i] = i < a.nseq ? (int32_t)items : INT32_MAX;
+        if (i >= a.nseq) continue;
         a.len[i] = len[b0 + i];
         a.keep[i] = keep[b0 + i];
+        const int64_t n = (std::min(len[b0 + i], keep[b0 + i]) + d.sb - 1) / d.sb;
+        items += v.H * (in_place ? n > 0 : (n + a.group - 1) / a.group);
       }
+      a.items = (int32_t)items;
+      if (items == 0) continue;
       hipError_t e = dv::launch_evict_select(a, st);
       if (e == hipSuccess) e = dv::launch_evict_move(a, st);
       if (e != hipSuccess) return dv::hip_fail(e, "eviction launch");

@@ -125,15 +125,18 @@ constexpr int kWeighTokens = 128;
 hipError_t launch_attend_weigh(const AttendArgs& a, hipStream_t s);
 
 // ---- dv_evict ----
+// A work item is a group of `group` blocks of the result of one head of one
+// sequence, or in place all of them; item[] counts those of earlier sequences.
 struct EvictArgs {
   QLayout s, d;
   int32_t* kept;
   int32_t kept_stride, recent, l0, nl;
   int32_t b0, nseq, in_place, most;  // most: tokens of the longest sequence
-  int32_t blocks, pad;  // most result blocks of a sequence
-  FastDiv d_du;          // by 16-code units of a token
+  int32_t blocks, group, items, pad;  // blocks: most result blocks of a sequence
+  FastDiv d_du;                       // by 16-code units of a token
   int32_t len[kQSeqs];
   int32_t keep[kQSeqs];
+  int32_t item[kQSeqs];  // INT32_MAX past the last
 };
 static_assert(sizeof(EvictArgs) <= 3584, "arguments stay under 4 KB");
 hipError_t launch_evict_select(const EvictArgs& a, hipStream_t s);

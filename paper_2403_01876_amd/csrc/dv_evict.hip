@@ -14,20 +14,26 @@ __device__ __forceinline__ uint32_t key_of(float w) {
 }
 
 // ---------------------------------------------------------------------------
-// A workgroup takes one head of one sequence.  The k-th largest key of the older
-// tokens is found a byte at a time from the top: a histogram of that byte over
-// the keys that agree with what is known, then the bin in which the k-th falls.
-// Keys above it stay, and of those equal to it the first ones; a pass over the
-// tokens in order counts both and writes slots, weights and positions.
-// The first kKeys * NT keys are held in registers, the others read each time.
+// Which tokens stay: a workgroup takes one head of one sequence.  The k-th largest
+// key of the older tokens is found a byte at a time from the top: a histogram of
+// that byte (one for each wave) over the keys that agree with what is known, then
+// the bin in which the k-th falls, until all of that bin stay or its keys are
+// equal.  Keys above it stay, and of those equal to it the first ones.  Then every
+// wave counts both in its tokens, and the counts before them place the tokens that
+// stay.
+// KH * NT weights at a time are in registers: of up to so many each is
+// read once, of more once for each histogram and once to place them.
+// Bound by latency: one round through memory, the rest in LDS.
 // ---------------------------------------------------------------------------
-constexpr int kKeys = 16;
+constexpr int kBins = 256;
 
-template <int NT>
+template <int NT, int KH>
 __global__ void __launch_bounds__(NT) evict_select_kernel(EvictArgs a) {
-  __shared__ int32_t hist[256];
-  __shared__ uint32_t found[2];  // the bin, and how many of it are wanted
-  __shared__ int2 counts[2][NT / 64];
+  constexpr int W = NT / 64;
+  __shared__ int32_t hist[W][kBins];
+  __shared__ int32_t sums[4];
+  __shared__ int32_t found[3];  // the bin, how many of it are wanted, its keys
+  __shared__ int2 counts[KH * W], totals;
   const int tid = threadIdx.x, l = tid & 63, wave = tid >> 6;
   const int b = blockIdx.x / (uint32_t)a.s.heads, h = blockIdx.x - b * a.s.heads, sb = a.b0 + b;
   const int layer = blockIdx.y;
@@ -35,50 +41,65 @@ __global__ void __launch_bounds__(NT) evict_select_kernel(EvictArgs a) {
   const int old = n - r, want = k - r;  // older tokens, and how many of them stay
   const int64_t row = ((int64_t)(a.l0 + layer) * a.s.batch + sb) * a.s.heads + h;
   const float* w = a.s.weight + row * a.s.cap;
+  if (k == 0) return;
 
-  uint32_t keys[kKeys];
-  if (want > 0 && want < old) {
+  float held[KH];
+  auto load = [&](int t0) {
 #pragma unroll
-    for (int i = 0; i < kKeys; ++i) keys[i] = i * NT + tid < old ? key_of(w[i * NT + tid]) : 0;
-  }
+    for (int i = 0; i < KH; ++i) {
+      held[i] = w[min(t0 + i * NT + tid, n - 1)];  // (no condition: all at once)
+    }
+  };
+  load(0);
+  const bool several = n > KH * NT;
   uint32_t line = 0;  // the want-th largest key, as far as it is known
   int equal = want;   // how many of the keys equal to it stay
-  if (want > 0 && want < old) {
+  const bool choose = want > 0 && want < old;
+  if (choose) {
     for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int i = tid; i < 256; i += NT) hist[i] = 0;
-      __syncthreads();
-      auto count = [&](uint32_t key) {
-        if (shift == 24 || key >> ((shift + 8) & 31) == line >> ((shift + 8) & 31))
-          atomicAdd(&hist[(key >> shift) & 255], 1);
-      };
 #pragma unroll
-      for (int i = 0; i < kKeys; ++i)
-        if (i * NT + tid < old) count(keys[i]);
-      for (int t = kKeys * NT + tid; t < old; t += NT) count(key_of(w[t]));
-      __syncthreads();
-      if (wave == 0) {  // lane l: bins 255 - 4 l and the three below
-        int32_t c[4], sum = 0;
+      for (int i = 0; i < kBins / 64; ++i) hist[wave][i * 64 + l] = 0;
+      for (int t0 = 0; t0 < old; t0 += KH * NT) {
+        if (several) load(t0);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum += c[i] = hist[255 - 4 * l - i];
-        int32_t above = sum;
+        for (int i = 0; i < KH; ++i) {
+          if (t0 + i * NT >= old) break;
+          const uint32_t key = key_of(held[i]);
+          const bool agrees = shift == 24 || (key ^ line) >> ((shift + 8) & 31) == 0;
+          if (t0 + i * NT + tid < old && agrees) atomicAdd(&hist[wave][(key >> shift) & 255], 1);
+        }
+      }
+      __syncthreads();
+      int32_t c = 0, above = 0;  // thread tid < 256: bin 255 - tid
+      if (tid < kBins) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) c += hist[i][kBins - 1 - tid];
+        above = c;
 #pragma unroll
         for (int x = 1; x < 64; x <<= 1) {
           const int32_t y = __shfl_up(above, x);
           if (l >= x) above += y;
         }
-        above -= sum;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (above < equal && equal <= above + c[i]) {
-            found[0] = 255 - 4 * l - i;
-            found[1] = equal - above;
-          }
-          above += c[i];
+        if (l == 63) sums[wave] = above;
+        above -= c;
+      }
+      __syncthreads();
+      if (tid < kBins) {
+        for (int i = 0; i < 4; ++i) above += i < wave ? sums[i] : 0;
+        if (above < equal && equal <= above + c) {
+          found[0] = kBins - 1 - tid;
+          found[1] = equal - above;
+          found[2] = c;
         }
       }
       __syncthreads();
-      line |= found[0] << shift;
+      line |= (uint32_t)found[0] << shift;
       equal = found[1];
+      if (equal == found[2] && line > 0) {  // all of the bin stay: the line lies below it
+        line -= 1;
+        equal = 0;
+        break;
+      }
     }
   }
 
@@ -86,54 +107,204 @@ __global__ void __launch_bounds__(NT) evict_select_kernel(EvictArgs a) {
   const int32_t* p = a.s.position ? a.s.position + row * a.s.cap : nullptr;
   float* dw = a.d.weight ? a.d.weight + row * a.d.cap : nullptr;
   int32_t* dp = a.d.position ? a.d.position + row * a.d.cap : nullptr;
-  int more = 0, same = 0;  // tokens before this step above the line, and on it
-  for (int t0 = 0, step = 0; t0 < n; t0 += NT, step ^= 1) {
-    const int t = t0 + tid;
-    const float wt = t < n ? w[t] : 0.f;
-    const int32_t pt = t < n && p ? p[t] : t;
-    bool up = t < n, on = false;
-    if (t < old) {
-      const uint32_t key = key_of(wt);
-      up = want == old || (want > 0 && key > line);
-      on = !up && want > 0 && key == line;
+  int more = 0, same = 0;  // tokens before this round above the line, and on it
+  for (int t0 = 0; t0 < n; t0 += KH * NT) {
+    if (several) load(t0);
+    int32_t pos[KH];
+    if (p && dp) {
+#pragma unroll
+      for (int i = 0; i < KH; ++i) {
+        pos[i] = p[min(t0 + i * NT + tid, n - 1)];
+      }
     }
-    const uint64_t ups = __ballot(up), ons = __ballot(on);
-    if (l == 0) counts[step][wave] = make_int2(__popcll(ups), __popcll(ons));
-    __syncthreads();  // and every load of this step is done: dst may be src
-    int before = more, level = same;
-    for (int i = 0; i < NT / 64; ++i) {
-      const int2 c = counts[step][i];
-      before += i < wave ? c.x : 0;
-      level += i < wave ? c.y : 0;
-      more += c.x;
-      same += c.y;
+    uint64_t ups[KH], ons[KH];
+#pragma unroll
+    for (int i = 0; i < KH; ++i) {
+      const int t = t0 + i * NT + tid;
+      const uint32_t key = key_of(held[i]);
+      const bool up = t < n && (t >= old || (choose ? key > line : want == old));
+      const bool on = t < old && choose && key == line;
+      ups[i] = __ballot(up);
+      ons[i] = __ballot(on);
+      if (l == 0) counts[i * W + wave] = make_int2(__popcll(ups[i]), __popcll(ons[i]));
     }
+    __syncthreads();  // and what this round reads has been read: dst may be src
+    if (wave == 0) {  // sums of the counts before each, a lane to each of 64 at a time
+      int x0 = more, y0 = same;
+#pragma unroll
+      for (int g = 0; g < KH * W; g += 64) {
+        const int2 c = g + l < KH * W ? counts[g + l] : make_int2(0, 0);
+        int x = c.x, y = c.y;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+          const int u = __shfl_up(x, o), v = __shfl_up(y, o);
+          if (l >= o) {
+            x += u;
+            y += v;
+          }
+        }
+        if (g + l < KH * W) counts[g + l] = make_int2(x0 + x - c.x, y0 + y - c.y);
+        x0 += __builtin_amdgcn_readlane(x, 63);
+        y0 += __builtin_amdgcn_readlane(y, 63);
+      }
+      if (l == 0) totals = make_int2(x0, y0);
+    }
+    __syncthreads();
+    more = totals.x;
+    same = totals.y;
     const uint64_t mine = (1ull << l) - 1;
-    before += __popcll(ups & mine);
-    level += __popcll(ons & mine);
-    if (up || (on && level < equal)) {
-      const int at = before + min(level, equal);
-      kept[at] = t;
-      if (dw) dw[at] = wt;
-      if (dp) dp[at] = pt;
+#pragma unroll
+    for (int i = 0; i < KH; ++i) {
+      const int t = t0 + i * NT + tid;
+      const int2 base = counts[i * W + wave];
+      const int level = base.y + __popcll(ons[i] & mine);
+      const bool up = (ups[i] >> l) & 1, on = (ons[i] >> l) & 1;
+      if (up || (on && level < equal)) {
+        const int at = base.x + __popcll(ups[i] & mine) + (choose ? min(level, equal) : 0);
+        kept[at] = t;
+        if (dw) dw[at] = held[i];
+        if (dp) dp[at] = p ? pos[i] : t;
+      }
     }
+    __syncthreads();
   }
 }
 
+// The largest magnitude of sixteen codes times their scale, and m; NaN is left out.
+__device__ __forceinline__ float amax_of(const u32x4& c, float scale, float m) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const f32x2 x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c[i], scale, false);
+    const f32x2 y = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c[i], scale, true);
+    m = fmaxf(m, fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(y[0]), fabsf(y[1]))));
+  }
+  return m;
+}
+// The codes of ratio times what sixteen codes stand for.
+__device__ __forceinline__ u32x4 again(u32x4 c, float ratio) {
+  ratio = fmaxf(ratio, 0x1p-126f);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const f32x2 x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c[i], ratio, false);
+    const f32x2 y = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c[i], ratio, true);
+    const int w = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
+    c[i] = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], w, true);
+  }
+  return c;
+}
+
 // ---------------------------------------------------------------------------
-// Codes and scales: a wave takes one block of the result.  Its tokens are read
-// (rows of head_dim bytes), the largest magnitude gives the new scale, and since
-// scales are powers of two the codes change only where a smaller one grows past
-// them.  In place a workgroup takes all of a head's blocks in order, four at a
-// time: a block's tokens come from its own slots or later ones, so once the four
-// waves have read, what they write over is no longer needed.  (A block too large
-// for a wave's registers is read again after its scale is known; in place such
-// blocks are taken one at a time, 64 units in order, which keeps that true.)
+// Codes and scales: a workgroup takes a group of blocks of the result, keys and
+// values.  It first looks up where each of their tokens lies and its scales (LDS),
+// then a wave takes a block of one half at a time: its tokens' rows come from
+// memory, the largest magnitude gives the new scale, and since scales are powers
+// of two the codes change only where a smaller one grows past them.  The next
+// block's rows are on their way meanwhile.
+// In place a workgroup takes all of a head's blocks in order, four at a time: a
+// block's tokens come from its own slots or later ones, so once the four waves
+// have read, what they write over is no longer needed.
 // Bound by HBM.
 // ---------------------------------------------------------------------------
-constexpr int kHeld = 4;
+constexpr int kHeld = 4;  // units of 16 codes that a lane holds: a block has 64 times as many
 
-__global__ void __launch_bounds__(kThreads) evict_move_kernel(EvictArgs a, int groups) {
+__global__ void __launch_bounds__(kThreads) evict_move_kernel(EvictArgs a) {
+  extern __shared__ uint32_t table[];  // place, key scale, value scale of a group's tokens
+  const int tid = threadIdx.x, l = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int below = 0;
+  for (int i = 0; i < a.nseq; i += 64)
+    below += __popcll(__ballot(a.item[i + l] <= (int)blockIdx.x));
+  const int b = __builtin_amdgcn_readfirstlane(below - 1), sb = a.b0 + b;
+  const int k = min(a.len[b], a.keep[b]);
+  const QLayout &s = a.s, &d = a.d;
+  const int blocks = d.d_bs.div(k + d.bs - 1);
+  const int groups = a.in_place ? 1 : (blocks + a.group - 1) / a.group;
+  const int item = (int)blockIdx.x - a.item[b];
+  const int h = __builtin_amdgcn_readfirstlane(item / groups), g0 = item - h * groups;
+  const int layer = blockIdx.y, du = s.D / 16, span = a.group * d.bs;
+  const int64_t slab = 2 * ((int64_t)a.l0 + layer);
+  const int32_t* kept = a.kept + (((int64_t)layer * a.s.batch + sb) * a.s.heads + h) *
+                                     a.kept_stride;
+  const uint8_t* from = s.codes + slab * s.s_slab + sb * s.s_b + h * s.s_h;
+  const float* from_scale = s.scale + slab * s.c_slab + sb * s.c_b + h * s.c_h;
+  uint8_t* to = d.codes + slab * d.s_slab + sb * d.s_b + h * d.s_h;
+  float* to_scale = d.scale + slab * d.c_slab + sb * d.c_b + h * d.c_h;
+  float* scales = (float*)table + span;
+
+  for (int g = g0; g * a.group < blocks; g += groups) {
+    const int j0 = g * a.group, tokens = min(span, k - j0 * d.bs);
+    for (int i = tid; i < tokens; i += kThreads) {
+      const int t = kept[j0 * d.bs + i], sj = s.d_bs.div(t);
+      int64_t blk = s.bt ? s.bt[(int64_t)sb * s.max_blocks + sj] : sj;
+      const bool hole = s.bt && (uint64_t)blk >= (uint64_t)s.num_blocks;
+      blk = hole ? 0 : blk;
+      table[i] = hole ? ~0u : (uint32_t)((blk * s.s_blk + (int64_t)(t - sj * s.bs) * s.D) >> 4);
+      scales[i] = from_scale[blk * s.c_blk];
+      scales[span + i] = from_scale[blk * s.c_blk + s.c_slab];
+    }
+    __syncthreads();
+    // jobs: blocks j0 + wave + 4 x, keys then values
+    struct Job {
+      u32x4 c[kHeld];
+      float scale[kHeld];
+    };
+    const int jobs = 2 * ((min(a.group, blocks - j0) + 3) / 4);
+    auto units_of = [&](int job) {
+      const int j = j0 + wave + 4 * (job >> 1);
+      return j < blocks ? min(d.bs, k - j * d.bs) * du : 0;
+    };
+    auto read = [&](Job& x, int job) {
+      const int first = (wave + 4 * (job >> 1)) * d.bs, units = units_of(job);
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) {
+        const int u = l + i * 64;
+        x.c[i] = u32x4{0, 0, 0, 0};
+        x.scale[i] = 1.f;
+        if (u < units) {
+          const int tok = a.d_du.div(u), part = u - tok * du;
+          const uint32_t at = table[first + tok];
+          if (at != ~0u)
+            x.c[i] = *(const u32x4*)(from + (job & 1) * s.s_slab + ((uint64_t)at + part) * 16);
+          x.scale[i] = scales[(job & 1) * span + first + tok];
+        }
+      }
+    };
+    auto write = [&](const Job& x, int job) {
+      const int j = j0 + wave + 4 * (job >> 1), units = units_of(job);
+      float m = 0.f;
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i)
+        if (i * 64 < units) m = amax_of(x.c[i], x.scale[i], m);
+#pragma unroll
+      for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+      if (units == 0) return;
+      const int64_t blk = d.bt ? d.bt[(int64_t)sb * d.max_blocks + j] : j;
+      if (d.bt && (uint64_t)blk >= (uint64_t)d.num_blocks) return;
+      const float p = scale_for(m), inv = inverse(p);
+      u32x4* out = (u32x4*)(to + (job & 1) * d.s_slab + blk * d.s_blk);
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i)
+        if (l + i * 64 < units)
+          __builtin_nontemporal_store(again(x.c[i], x.scale[i] * inv), out + l + i * 64);
+      if (l == 0) to_scale[(job & 1) * d.c_slab + blk * d.c_blk] = p;
+    };
+    Job x, y;
+    read(x, 0);
+    for (int job = 0; job < jobs; job += 2) {  // jobs are even
+      read(y, job + 1);
+      if (a.in_place) __syncthreads();  // all four waves have read their two blocks
+      write(x, job);
+      if (job + 2 < jobs) read(x, job + 2);
+      write(y, job + 1);
+    }
+    __syncthreads();
+  }
+}
+
+// The same for blocks too large to be held, read again after their scale is known.
+// In place a workgroup is one wave and takes a head's blocks in order, 64 units of
+// a block in order: what it writes over has been read.
+__global__ void __launch_bounds__(kThreads) evict_move_large_kernel(EvictArgs a, int groups) {
   const int l = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   const int g = blockIdx.x % (uint32_t)groups, bh = blockIdx.x / (uint32_t)groups;
   const int b = bh / a.s.heads, h = bh - b * a.s.heads, sb = a.b0 + b;
@@ -148,7 +319,6 @@ __global__ void __launch_bounds__(kThreads) evict_move_kernel(EvictArgs a, int g
   uint8_t* to = d.codes + slab * d.s_slab + sb * d.s_b + h * d.s_h;
   float* to_scale = d.scale + slab * d.c_slab + sb * d.c_b + h * d.c_h;
   const int du = s.D / 16, blocks = d.d_bs.div(k + d.bs - 1);
-
   // Sixteen codes of unit u of the result's block j, and their scale.
   auto read = [&](int j, int u, float* scale) {
     const int tok = a.d_du.div(u), part = u - tok * du;
@@ -159,88 +329,53 @@ __global__ void __launch_bounds__(kThreads) evict_move_kernel(EvictArgs a, int g
     *scale = from_scale[blk * s.c_blk];
     return *(const u32x4*)(from + blk * s.s_blk + (int64_t)(t - sj * s.bs) * s.D + part * 16);
   };
-  auto amax = [&](const u32x4& c, float scale, float m) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const f32x2 x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c[i], scale, false);
-      const f32x2 y = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c[i], scale, true);
-      m = fmaxf(m, fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(y[0]), fabsf(y[1]))));
-    }
-    return m;
-  };
-  auto again = [&](u32x4 c, float ratio) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const f32x2 x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c[i], ratio, false);
-      const f32x2 y = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c[i], ratio, true);
-      const int w = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
-      c[i] = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], w, true);
-    }
-    return c;
-  };
-
-  const int step = groups * waves;
-  for (int j0 = g * waves; j0 < blocks; j0 += step) {
-    const int j = j0 + wave;
-    const int units = j < blocks ? min(d.bs, k - j * d.bs) * du : 0;
-    u32x4 c[kHeld];
-    float scale[kHeld], m = 0.f;
-#pragma unroll
-    for (int i = 0; i < kHeld; ++i) {
-      const int u = l + i * 64;
-      c[i] = u32x4{0, 0, 0, 0};
-      scale[i] = 1.f;
-      if (u < units) c[i] = read(j, u, &scale[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < kHeld; ++i) m = amax(c[i], scale[i], m);
-    for (int u = l + kHeld * 64; u < units; u += 64) {
-      float x;
-      const u32x4 y = read(j, u, &x);
-      m = amax(y, x, m);
+  for (int j = g * waves + wave; j < blocks; j += groups * waves) {
+    const int units = min(d.bs, k - j * d.bs) * du;
+    float m = 0.f, x;
+    for (int u = l; u < units; u += 64) {
+      const u32x4 c = read(j, u, &x);
+      m = amax_of(c, x, m);
     }
 #pragma unroll
     for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-    if (a.in_place) __syncthreads();
-    int64_t blk = 0;
-    bool hole = units == 0;
-    if (!hole) {
-      blk = d.bt ? d.bt[(int64_t)sb * d.max_blocks + j] : j;
-      hole = d.bt && (uint64_t)blk >= (uint64_t)d.num_blocks;
+    const int64_t blk = d.bt ? d.bt[(int64_t)sb * d.max_blocks + j] : j;
+    if (d.bt && (uint64_t)blk >= (uint64_t)d.num_blocks) continue;
+    const float p = scale_for(m), inv = inverse(p);
+    u32x4* out = (u32x4*)(to + blk * d.s_blk);
+    for (int u = l; u < units; u += 64) {
+      const u32x4 c = read(j, u, &x);
+      out[u] = again(c, x * inv);
     }
-    if (!hole) {
-      const float p = scale_for(m), inv = inverse(p);
-      u32x4* out = (u32x4*)(to + blk * d.s_blk);
-#pragma unroll
-      for (int i = 0; i < kHeld; ++i)
-        if (l + i * 64 < units) out[l + i * 64] = again(c[i], fmaxf(scale[i] * inv, 0x1p-126f));
-      for (int u = l + kHeld * 64; u < units; u += 64) {
-        float x;
-        const u32x4 y = read(j, u, &x);
-        out[u] = again(y, fmaxf(x * inv, 0x1p-126f));
-      }
-      if (l == 0) to_scale[blk * d.c_blk] = p;
-    }
-    if (a.in_place) __syncthreads();
+    if (l == 0) to_scale[blk * d.c_blk] = p;
   }
 }
 
 }  // namespace
 
 hipError_t launch_evict_select(const EvictArgs& a, hipStream_t s) {
-  const bool wide = a.most > kKeys * 256;
-  const void* fn = wide ? (const void*)&evict_select_kernel<1024>
-                        : (const void*)&evict_select_kernel<256>;
+  // As few weights to a lane as hold the longest sequence.
+  const bool wide = a.most > 16 * 256;
+  const void* fn = wide                ? (const void*)&evict_select_kernel<1024, 16>
+                   : a.most > 4 * 256 ? (const void*)&evict_select_kernel<256, 16>
+                                      : (const void*)&evict_select_kernel<256, 4>;
   void* args[] = {const_cast<EvictArgs*>(&a)};
   return hipLaunchKernel(fn, dim3((uint32_t)a.nseq * a.s.heads, a.nl), dim3(wide ? 1024 : 256),
                          args, 0, s);
 }
 
+bool evict_blocks_held(int64_t bs, int64_t D) { return bs * D <= kHeld * 1024; }
+
 hipError_t launch_evict_move(const EvictArgs& a, hipStream_t s) {
-  const int waves = a.in_place && (int64_t)a.s.bs * a.s.D > kHeld * 1024 ? 1 : 4;
+  EvictArgs x = a;
+  if (evict_blocks_held(a.d.bs, a.s.D)) {
+    void* args[] = {&x};
+    return hipLaunchKernel((const void*)&evict_move_kernel, dim3((uint32_t)a.items, a.nl),
+                           dim3(kThreads), args, (size_t)a.group * a.d.bs * 12, s);
+  }
+  const int waves = a.in_place ? 1 : 4;
   int groups = a.in_place ? 1 : (a.blocks + waves - 1) / waves;
-  void* args[] = {const_cast<EvictArgs*>(&a), &groups};
-  return hipLaunchKernel((const void*)&evict_move_kernel,
+  void* args[] = {&x, &groups};
+  return hipLaunchKernel((const void*)&evict_move_large_kernel,
                          dim3((uint32_t)a.nseq * a.s.heads * groups, 2 * a.nl), dim3(waves * 64),
                          args, 0, s);
 }
