@@ -89,7 +89,7 @@ typedef struct dv_attend_args {
   float scale;      /* the scores' factor, e.g. 1/sqrt(head_dim) */
   float decay;      /* with `weigh`: factor of the weights from before */
   int32_t weigh;    /* nonzero: accumulate into the cache's weight array */
-  int32_t reserved; /* 0 */
+  int32_t rows;     /* rows that q, out and lse have: at least the sum of q_len */
   const void* q;
   void* out;
   int64_t q_token, q_head, out_token, out_head; /* strides */
@@ -123,7 +123,7 @@ DV_API int dv_attend_bytes(const dv_quant* c, const int32_t* q_len, const int32_
  * its table are not written; out, lse, workspace and weights must not overlap
  * them nor each other (q and out, lse, workspace are checked as one contiguous
  * range each only where the strides make them one).
- * DV_OK, DV_ERR_INVALID, DV_ERR_RANGE, DV_ERR_SPACE (workspace too small),
+ * DV_OK, DV_ERR_INVALID, DV_ERR_RANGE, DV_ERR_SPACE (workspace or rows too few),
  * DV_ERR_UNSUPPORTED, DV_ERR_HIP. */
 DV_API int dv_attend(const dv_quant* c, int32_t mb, int32_t layer, const int32_t* q_len,
                      const int32_t* kv_len, const dv_attend_args* a, void* stream);

@@ -30,7 +30,7 @@ class dv_quant(ctypes.Structure):
 
 class dv_attend_args(ctypes.Structure):
     _fields_ = [("type", _i32_t), ("q_heads", _i32_t), ("scale", _f32), ("decay", _f32),
-                ("weigh", _i32_t), ("reserved", _i32_t), ("q", _vp), ("out", _vp),
+                ("weigh", _i32_t), ("rows", _i32_t), ("q", _vp), ("out", _vp),
                 ("q_token", _i64), ("q_head", _i64), ("out_token", _i64), ("out_head", _i64),
                 ("slopes", _vp), ("lse", _vp), ("workspace", _vp), ("workspace_bytes", _u64)]
 
@@ -51,6 +51,9 @@ for _name, _args in {
     _f = getattr(lib, _name)
     _f.argtypes = _args
     _f.restype = ctypes.c_int
+
+
+_attend, _byref = lib.dv_attend, ctypes.byref
 
 
 class QuantCache:
@@ -100,11 +103,19 @@ def dv_quant_in(dst: QuantCache, mb: int, l0: int, l1: int, t0, t1, src, src_byt
 
 
 def _rows(name: str, x, dim: int):
-    """A [tokens, heads, head_dim] tensor's type, heads and strides."""
-    if x.dim() != 3 or x.shape[2] != dim or x.stride(2) != 1 or x.dtype not in _TYPES:
+    """A [tokens, heads, head_dim] tensor's tokens, heads and strides."""
+    shape, strides = x.shape, x.stride()
+    if len(shape) != 3 or shape[2] != dim or strides[2] != 1 or x.dtype not in _TYPES:
         raise ValueError(f"{name} must be a float16 or bfloat16 tensor [tokens, heads, {dim}] "
-                         f"with contiguous rows, got {tuple(x.shape)} {x.dtype}")
-    return x.stride(0), x.stride(1)
+                         f"with contiguous rows, got {tuple(shape)} {x.dtype}")
+    return shape[0], shape[1], strides[0], strides[1]
+
+
+def _floats(name: str, x, shape):
+    if x.dtype is not torch.float32 or x.dim() != len(shape) or x.shape[-1] != shape[-1] or \
+            not x.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous float32 tensor of {shape}, got "
+                         f"{tuple(x.shape)} {x.dtype}")
 
 
 def dv_attend_bytes(c: QuantCache, q_len, kv_len, q, weights: bool = False,
@@ -130,26 +141,26 @@ def dv_attend(c: QuantCache, mb: int, layer: int, q_len, kv_len, q, out, scale: 
     the cache's weights, those from before times this (None: do not).  ``lse``: a
     float32 [tokens, q_heads] tensor.  ``workspace``: a tensor of dv_attend_bytes
     bytes."""
-    batch = c.cache.c.batch
-    a0, p0 = _i32(q_len, batch)
-    a1, p1 = _i32(kv_len, batch)
-    qt, qh = _rows("q", q, c.cache.c.head_dim)
-    ot, oh = _rows("out", out, c.cache.c.head_dim)
-    n = int(a0[:batch].sum())
-    if q.shape[0] < n or out.shape[0] < n or out.shape[1] != q.shape[1] or out.dtype != q.dtype:
-        raise ValueError(f"{n} queries, q {tuple(q.shape)} {q.dtype}, "
-                         f"out {tuple(out.shape)} {out.dtype}")
-    for name, x, shape in (("slopes", slopes, (q.shape[1],)), ("lse", lse, (n, q.shape[1]))):
-        if x is not None and (x.dtype != torch.float32 or not x.is_contiguous() or
-                              x.shape[-1] != q.shape[1] or x.numel() < shape[0] * (
-                                  q.shape[1] if name == "lse" else 1)):
-            raise ValueError(f"{name} must be a contiguous float32 tensor of {shape}, got "
-                             f"{tuple(x.shape)} {x.dtype}")
+    cache = c.cache.c
+    a0, p0 = _i32(q_len, cache.batch)
+    a1, p1 = _i32(kv_len, cache.batch)
+    rows, heads, qt, qh = _rows("q", q, cache.head_dim)
+    out_rows, out_heads, ot, oh = _rows("out", out, cache.head_dim)
+    if out_heads != heads or out.dtype is not q.dtype:
+        raise ValueError(f"q {tuple(q.shape)} {q.dtype}, out {tuple(out.shape)} {out.dtype}")
+    if out_rows < rows:
+        rows = out_rows
+    if slopes is not None:
+        _floats("slopes", slopes, (heads,))
+        slopes = slopes.data_ptr()
+    if lse is not None:
+        _floats("lse", lse, (min(rows, lse.shape[0]), heads))
+        rows, lse = min(rows, lse.shape[0]), lse.data_ptr()
     wb = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    a = dv_attend_args(_TYPES[q.dtype], q.shape[1], scale, 0.0 if decay is None else decay,
-                       decay is not None, 0, q.data_ptr(), out.data_ptr(), qt, qh, ot, oh,
-                       _addr(slopes), _addr(lse), _addr(workspace), wb)
-    rc = lib.dv_attend(c.ref, mb, layer, p0, p1, ctypes.byref(a), _stream(stream))
+    a = dv_attend_args(_TYPES[q.dtype], heads, scale, 0.0 if decay is None else decay,
+                       decay is not None, rows, q.data_ptr(), out.data_ptr(), qt, qh, ot, oh,
+                       slopes, lse, _addr(workspace), wb)
+    rc = _attend(c.ref, mb, layer, p0, p1, _byref(a), _stream(stream))
     return _check(rc, "dv_attend", check)
 
 

@@ -143,6 +143,20 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// The sum over the 32 lanes of a half wave, in all of them: a row of 16 by
+// rotations, then the two rows.
+__device__ __forceinline__ float sum_of_half(float x) {
+  auto turned = [](float v, auto by) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x120 + decltype(by)::value,
+                                                      0xf, 0xf, false));  // row_ror
+  };
+  x += turned(x, std::integral_constant<int, 8>{});
+  x += turned(x, std::integral_constant<int, 4>{});
+  x += turned(x, std::integral_constant<int, 2>{});
+  x += turned(x, std::integral_constant<int, 1>{});
+  return x + __shfl_xor(x, 16);
+}
+
 // 0x80 in each byte of w that is a NaN code.
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
   return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
@@ -171,6 +185,47 @@ __device__ __forceinline__ void spread_nan(const AttendArgs& a, int sb, int h, i
       part[(int64_t)r * DP + d] = NAN;
     else
       ((uint16_t*)a.out)[(int64_t)(tok + i) * a.o_token + (int64_t)head * a.o_head + d] = 0x7fff;
+  }
+}
+
+// The weights of a chunk's tokens [c0, c0 + cn) from the scores that were kept, four
+// tokens to a lane, and its nr rows' lse2 (in LDS).  Short chunks deal the rows to
+// as many groups of lanes as there are, whose sums are added in order (`part`, 4 KB
+// of LDS).
+__device__ __forceinline__ void add_weights(const AttendArgs& a, const Seq& seq, int sb, int h,
+                                            int nr, int c0, int cn, const float* lse2s,
+                                            f32x4* part) {
+  const QLayout& q = a.q;
+  const int64_t pitch = (seq.len + 31) & ~31;
+  const float* sc = a.scores + (int64_t)a.soff[seq.b] * 32 + (int64_t)h * nr * pitch;
+  float* weight = q.weight + (((int64_t)a.layer * q.batch + sb) * q.heads + h) * (int64_t)q.cap;
+  const int tid = threadIdx.x;
+  int lanes = kThreads;
+  while (lanes > 32 && lanes * 2 >= cn) lanes >>= 1;  // half as many still cover the chunk
+  const int groups = kThreads / lanes, group = tid / lanes, lane = tid & (lanes - 1);
+  for (int t0 = 0; t0 < cn; t0 += lanes * 4) {  // (scores are padded to 32 tokens)
+    const int t = t0 + lane * 4;
+    f32x4 w = {0, 0, 0, 0};
+    if (t < cn) {
+#pragma unroll 8
+      for (int r = group; r < nr; r += groups) {
+        const f32x4 s2 = *(const f32x4*)(sc + r * pitch + c0 + t);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)  // hidden tokens get 0 also where lse is NaN
+          w[i] += s2[i] == -INFINITY ? 0.f : exp2_(s2[i] - lse2s[r]);
+      }
+    }
+    if (groups > 1) {  // (one step: the lanes of a group cover the chunk)
+      part[tid] = w;
+      __syncthreads();
+      for (int g = 1; g < groups; ++g) w += part[g * lanes + lane];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (group == 0 && t + i < cn) {
+        float* to = weight + c0 + t + i;
+        *to = a.decay == 0.f ? w[i] : a.decay * *to + w[i];
+      }
   }
 }
 
@@ -569,6 +624,20 @@ __global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
   }
   nan_from = min(min(nans[0], nans[2]), min(nans[4], nans[6]));
   nan_to = max(max(nans[1], nans[3]), max(nans[5], nans[7]));
+  if (direct && a.weigh) {  // the workgroup's own scores are all there are
+    float* lse2s = sums;
+    wait_loads<0>();
+    __syncthreads();
+    if (tid < rows) {
+      float top = kLow, total = 0.f;
+      for (int w = 0; w < 4; ++w) top = fmaxf(top, mls[(w * RT * 16 + tid) * 2]);
+      for (int w = 0; w < 4; ++w)
+        total += mls[(w * RT * 16 + tid) * 2 + 1] * exp2_(mls[(w * RT * 16 + tid) * 2] - top);
+      lse2s[tid] = total == 0.f ? INFINITY : top + __log2f(total);
+    }
+    __syncthreads();
+    add_weights(a, seq, sb, h, rows, c0, cn, lse2s, (f32x4*)(sums + 64));
+  }
   if (nan_from < nan_to) {
     wait_loads<0>();
     __syncthreads();
@@ -1069,27 +1138,9 @@ __global__ void __launch_bounds__(kThreads) attend_join_kernel(AttendArgs a, int
     for (int x = 16; x; x >>= 1) sum += __shfl_xor(sum, x);
     if (tid % 32 == 0) lse2s[r] = sum == 0.f ? INFINITY : up + __log2f(sum);
   }
-  const int64_t pitch = (len + 31) & ~31;
-  const float* sc = a.scores + (int64_t)a.soff[b] * 32 + (int64_t)h * rows * pitch;
-  float* weight = q.weight + (((int64_t)a.layer * q.batch + sb) * q.heads + h) * (int64_t)q.cap;
-  const int c0 = split * a.chunk, cn = min(a.chunk, len - c0);
   __syncthreads();
-  for (int t = tid * 4; t < cn; t += kThreads * 4) {  // the scores are padded to 32 tokens
-    f32x4 w = {0, 0, 0, 0};
-#pragma unroll 8
-    for (int r = 0; r < nr; ++r) {
-      const f32x4 s2 = *(const f32x4*)(sc + r * pitch + c0 + t);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)  // hidden tokens get 0 also where lse is NaN
-        w[i] += s2[i] == -INFINITY ? 0.f : exp2_(s2[i] - lse2s[r]);
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (t + i < cn) {
-        float* to = weight + c0 + t + i;
-        *to = a.decay == 0.f ? w[i] : a.decay * *to + w[i];
-      }
-  }
+  add_weights(a, seq, sb, h, nr, split * a.chunk, min(a.chunk, len - split * a.chunk), lse2s,
+              (f32x4*)acc);
 }
 
 // ---------------------------------------------------------------------------
@@ -1241,8 +1292,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 3 : 1) attend_weigh_kern
   for (int u = 0; u < 2; ++u)
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-#pragma unroll
-      for (int x = 16; x; x >>= 1) sum[u][i] += __shfl_xor(sum[u][i], x);
+      sum[u][i] = sum_of_half(sum[u][i]);
       if (odd && c == i) part[wave & 1][u * 32 + (i / 4) * 8 + hf * 4 + i % 4] = sum[u][i];
     }
   __syncthreads();

@@ -186,16 +186,19 @@ int plan_of(const Quant& q, const int32_t* q_len, const int32_t* kv_len, const d
     p->R = most <= 16 ? 16 : most <= 32 ? 32 : 64;
     // The smallest chunk whose work items the card holds all at once.
     const int64_t round = dv::kSplitRound;
-    int64_t chunk = std::max<int64_t>(1, total / 1024 / round) * round;
+    uint32_t chunk = (uint32_t)(std::max<int64_t>(1, total / 1024 / round) * round);
     for (; chunk < dv::kSplitChunkMax; chunk += round) {
-      int64_t items = 0;
+      uint32_t splits = 0;
       for (int64_t b = 0; b < v.B; ++b)
-        if (q_len[b] > 0) items += std::max<int64_t>(1, (kv_len[b] + chunk - 1) / chunk) * v.H;
-      if (items <= 256 * dv::split_groups((int)p->Dp, p->R / 16, (int)chunk, a->slopes != nullptr))
+        if (q_len[b] > 0) splits += kv_len[b] ? ((uint32_t)kv_len[b] + chunk - 1) / chunk : 1;
+      if (splits * v.H <=
+          256 * dv::split_groups((int)p->Dp, p->R / 16, (int)chunk, a->slopes != nullptr))
         break;
     }
-    if (longest <= 2 * round) chunk = std::max(chunk, (longest + round - 1) / round * round);
-    p->chunk = (int32_t)std::min<int64_t>(std::max(chunk, round), dv::kSplitChunkMax);
+    // (Up to two rounds of four waves are not worth joining.)
+    int64_t most_split = longest <= 2 * round ? (longest + round - 1) / round * round : 0;
+    most_split = std::max<int64_t>(std::max<int64_t>(most_split, chunk), round);
+    p->chunk = (int32_t)std::min<int64_t>(most_split, dv::kSplitChunkMax);
   } else {
     p->R = dv::kTileRows;
     int64_t tiles = 0;
@@ -204,7 +207,7 @@ int plan_of(const Quant& q, const int32_t* q_len, const int32_t* kv_len, const d
     if (tiles < 512) chunk = std::max<int64_t>(512, longest * tiles / 512);
     p->chunk = (int32_t)std::max<int64_t>(64, (chunk + 63) & ~63ll);
   }
-  p->direct = longest <= p->chunk && !(p->split && a->weigh);
+  p->direct = longest <= p->chunk;
   // Workspace of the largest launch; they run one after another.
   p->part = p->ml = p->scores = p->lse = 0;
   for (int64_t b0 = 0; b0 < v.B; b0 += kQSeqs) {
@@ -261,9 +264,10 @@ int attend(const dv_quant* c, int32_t mb, int32_t layer, const int32_t* q_len,
   Plan p;
   rc = plan_of(q, q_len, kv_len, u, &p);
   if (rc != DV_OK) return rc;
-  if (u->reserved != 0 || (u->weigh && !q.weight)) return DV_ERR_INVALID;
+  if (u->weigh && !q.weight) return DV_ERR_INVALID;
   int64_t tokens = 0;
   for (int64_t b = 0; b < v.B; ++b) tokens += q_len[b];
+  if (u->rows < tokens) return DV_ERR_SPACE;
   if (tokens == 0) return DV_OK;
   const int64_t D = v.D;
   const int64_t strides[4] = {u->q_token, u->q_head, u->out_token, u->out_head};

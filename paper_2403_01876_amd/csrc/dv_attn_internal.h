@@ -103,7 +103,7 @@ constexpr int split_queries(int DP, int RT) { return RT == 4 ? RT * DP * 32 : 0;
 // a CU, its bytes of LDS (the codes of a step of four waves and the tables of a
 // chunk, or the waves' results) and those that both allow.
 constexpr int split_waves(int DP, int RT) {
-  return DP <= 64 ? (RT == 1 ? 4 : RT == 2 ? 3 : 2) : DP <= 128 ? (RT == 1 ? 3 : 2) : 1;
+  return DP <= 64 ? (RT == 1 ? 4 : RT == 2 ? 3 : 2) : DP <= 128 ? (RT == 1 ? 3 : 2) : RT == 1 ? 2 : 1;
 }
 inline size_t split_lds(int DP, int rt, int chunk, bool slopes) {
   const size_t tables = (size_t)4 * 2 * kSplitStep * DP + split_queries(DP, rt) +
