@@ -16,6 +16,7 @@
 // at most, which costs no precision.  kLift is 7 for f16, whose probabilities stay
 // normal numbers down to 2^-21 of the largest so (a value 2^12 times another's
 // shows their rounding below 2^-14 otherwise), and 0 for bf16.
+#include <algorithm>
 #include <type_traits>
 
 #include "dv_attn_internal.h"
@@ -689,7 +690,7 @@ struct TileLds {
 };
 
 template <bool BF16, int DP>
-__global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1)
+__global__ void __launch_bounds__(kThreads, tile_waves(DP))
     attend_tile_kernel(AttendArgs a, int direct) {
   using T = Ty<BF16>;
   using L = TileLds<DP>;
@@ -1041,11 +1042,17 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1)
 
 // ---------------------------------------------------------------------------
 // Joins the splits of the kernels above: R rows a work item, a workgroup for each
-// split of a head.  Grid row 0 adds up the results: four dims to a lane, a group
-// of lanes to a row; up to 16 splits are one group's, more are dealt to all of a
-// workgroup's groups.  Grid row 1, where the scores were kept, adds up the
-// weights of the split's own tokens, four to a lane, for which it needs every
-// row's sum.  Bound by latency: two rounds through memory.
+// split of a head and 32 of its rows (64 rows: 45.0 us with the split kernel, with
+// one workgroup 46.9; 128: 104 and 106).  They add up the results: four dims to a
+// lane, a group of lanes to a row.  Up to 16 splits are one group's where there
+// are more rows than splits; more, or of few rows, are dealt to all of a
+// workgroup's groups (8 rows of 14 splits: 14.9 us instead of 16.3 with the split
+// kernel; 16 rows of 4: 38.5 instead of 24.5).  The last row of the grid,
+// where the scores were kept, adds up the weights of the split's own tokens, four to a lane, for which
+// it needs every row's sum.
+// Bound by latency: two rounds through memory.  4 to 5 us a decode step, of which
+// 2 are the launch; 15 us where it reads 34 MB of scores (131071 tokens, 8 heads
+// of 8 queries).
 // ---------------------------------------------------------------------------
 template <bool BF16, int DP>
 __global__ void __launch_bounds__(kThreads) attend_join_kernel(AttendArgs a, int R) {
@@ -1066,10 +1073,11 @@ __global__ void __launch_bounds__(kThreads) attend_join_kernel(AttendArgs a, int
   const int r0 = tile * R, nr = min(R, rows - r0);
   const float2* ml = (const float2*)a.ml + ((int64_t)item - split) * R;
 
-  if (blockIdx.y == 0) {
-    const bool alone = nsplit <= kAlone;
+  const int shares = gridDim.y - (a.scores ? 1 : 0), share = blockIdx.y;
+  if (share < shares) {
+    const bool alone = nsplit <= 2 || (nsplit <= kAlone && nr > nsplit);
     const int group = tid / DL, d = tid % DL * 4, per = alone ? P : 1;
-    for (int rb = split * per; rb < nr; rb += nsplit * per) {
+    for (int rb = (share * nsplit + split) * per; rb < nr; rb += shares * nsplit * per) {
       const int r = min(alone ? rb + group : rb, nr - 1);
       const float* part = a.part + (((int64_t)item - split) * R + r) * DP + d;
       f32x4 v = {0, 0, 0, 0};
@@ -1362,7 +1370,7 @@ hipError_t launch_attend_tile(const AttendArgs& a, bool direct, hipStream_t s) {
 
 hipError_t launch_attend_join(const AttendArgs& a, int rows, hipStream_t s) {
   return launch(pick(a, [](auto k) { return decltype(k)::join(); }),
-                dim3(a.items, a.weigh && a.scores ? 2 : 1), 0, s, a, rows);
+                dim3(a.items, std::max(1, rows / 32) + (a.scores ? 1 : 0)), 0, s, a, rows);
 }
 
 hipError_t launch_attend_weigh(const AttendArgs& a, hipStream_t s) {

@@ -142,7 +142,12 @@ int64_t blocks_of(const Quant& q, int64_t t0, int64_t t1) {
 
 // ---- dv_attend ------------------------------------------------------------------------------
 
-constexpr int64_t kFewRows = 64, kFewRowsWide = 32;  // the second for head_dim above 128
+// Rows (queries and heads of a group) up to which the split kernel takes a call,
+// the second for head_dim above 128: as many as its registers hold, since it is
+// faster up to there.  16 sequences of 128 to 4096 tokens, 8 heads: 16 rows 24.5 us
+// instead of 50.7, 64 rows 45 instead of 57; head_dim 256, 4 heads, 32 rows 35
+// instead of 80.
+constexpr int64_t kFewRows = 64, kFewRowsWide = 32;
 
 // How a call's work is divided, and its workspace.
 struct Plan {
@@ -184,7 +189,9 @@ int plan_of(const Quant& q, const int32_t* q_len, const int32_t* kv_len, const d
   p->split = most <= (p->Dp == 256 ? kFewRowsWide : kFewRows);
   if (p->split) {
     p->R = most <= 16 ? 16 : most <= 32 ? 32 : 64;
-    // The smallest chunk whose work items the card holds all at once.
+    // The smallest chunk whose work items the card holds all at once: 32 sequences
+    // of 128 to 4096 tokens, 8 heads 32 us; half as many items 38.8, 1.5, 2 and 3
+    // times as many 39.4, 35.4 and 40.6.
     const int64_t round = dv::kSplitRound;
     uint32_t chunk = (uint32_t)(std::max<int64_t>(1, total / 1024 / round) * round);
     for (; chunk < dv::kSplitChunkMax; chunk += round) {
@@ -195,17 +202,35 @@ int plan_of(const Quant& q, const int32_t* q_len, const int32_t* kv_len, const d
           256 * dv::split_groups((int)p->Dp, p->R / 16, (int)chunk, a->slopes != nullptr))
         break;
     }
-    // (Up to two rounds of four waves are not worth joining.)
+    // (Up to two rounds of four waves are not worth joining: 250 tokens 9.7 us,
+    // joined 11.7; 400 tokens in one chunk 13.1, joined 12.4.)
     int64_t most_split = longest <= 2 * round ? (longest + round - 1) / round * round : 0;
     most_split = std::max<int64_t>(std::max<int64_t>(most_split, chunk), round);
     p->chunk = (int32_t)std::min<int64_t>(most_split, dv::kSplitChunkMax);
   } else {
     p->R = dv::kTileRows;
-    int64_t tiles = 0;
-    for (int64_t b = 0; b < v.B; ++b) tiles += (q_len[b] * G + p->R - 1) / p->R * v.H;
-    int64_t chunk = longest;
-    if (tiles < 512) chunk = std::max<int64_t>(512, longest * tiles / 512);
-    p->chunk = (int32_t)std::max<int64_t>(64, (chunk + 63) & ~63ll);
+    // The longest sequence in as many parts, of 256 tokens or more, as leave all
+    // work items at once on the card: 4000 tokens under 8 tiles of 8 heads 42.5 us
+    // in eight parts, 75 in four, 127 in one; under 32 tiles 104 in two, 128 in
+    // one; but under 50 tiles 166 in one, 187 in three and 276 in two uneven ones.
+    // (Up to 512 tokens are not worth joining: 500 tokens 24 us, in two parts 29.)
+    const int64_t slots = 256 * dv::tile_waves((int)p->Dp);
+    const auto tiles = [&](int64_t b) { return (q_len[b] * G + p->R - 1) / p->R * v.H; };
+    const auto chunk_of = [&](int64_t n) {
+      return std::max<int64_t>(64, ((longest + n - 1) / n + 63) / 64 * 64);
+    };
+    const auto items = [&](int64_t chunk) {
+      int64_t sum = 0;
+      for (int64_t b = 0; b < v.B; ++b)
+        sum += tiles(b) * std::max<int64_t>(1, (kv_len[b] + chunk - 1) / chunk);
+      return sum;
+    };
+    int64_t work = 0;
+    for (int64_t b = 0; b < v.B; ++b) work += tiles(b) * kv_len[b];
+    int64_t n = longest <= 512 ? 1 : (longest + 255) / 256;
+    n = std::min(n, longest * slots / std::max<int64_t>(1, work));
+    while (n > 1 && items(chunk_of(n)) > slots) --n;
+    p->chunk = (int32_t)chunk_of(std::max<int64_t>(1, n));
   }
   p->direct = longest <= p->chunk;
   // Workspace of the largest launch; they run one after another.
@@ -397,10 +422,14 @@ int dv_quant_in(const dv_quant* dst, int32_t mb, int32_t l0, int32_t l1, const i
   a.q = layout_args(q);
   a.w_slab = v.H * v.D * 2 * N;
   a.bf16 = type == DV_BF16;
-  // As many lanes to a block as its 16-element units ask for: one token of 128
-  // dimensions 8, a block of 16 of them 64 (two units a lane).
+  // As few lanes to a block as hold its 16-element units in registers, two each,
+  // or four where 64 lanes would not do: with 16 tokens of 128 dimensions (128
+  // units) a pool of 32 x 128 to 4096 tokens (two layers of 8 heads) takes 162 us,
+  // with room for four 165, and with that room and half of it empty 204; with 64
+  // tokens (512 units) four take 174 and two, which read most units again, 190.
   const int64_t units = std::min<int64_t>(a.q.bs, longest) * v.D / 16;
-  while (a.lanes_log2 < 6 && (1 << a.lanes_log2) < units) ++a.lanes_log2;
+  a.held = units <= 128 ? 2 : 4;
+  while (a.lanes_log2 < 6 && (a.held << a.lanes_log2) < units) ++a.lanes_log2;
   for (int32_t l = l0; l < l1; l += kLayers) {
     const int32_t nl = std::min(kLayers, l1 - l);
     int64_t tok = 0;

@@ -48,13 +48,14 @@ __device__ __forceinline__ float inverse(float p) {
 
 // ---- dv_quant_in ----
 // A work item is one block of one head of one sequence; item[] counts those of
-// earlier sequences.  A group of 1 << lanes_log2 lanes takes an item.
+// earlier sequences.  A group of 1 << lanes_log2 lanes takes an item, and each of
+// them holds `held` (2 or 4) units of 16 elements in registers.
 struct QuantArgs {
   QLayout q;
   const uint8_t* wire;  // advanced to this launch's first sequence
   int64_t w_slab;       // wire bytes per slab (layer, half)
   int32_t slab0, b0, nseq, items;
-  int32_t lanes_log2, bf16;
+  int32_t lanes_log2, held, bf16;
   int32_t item[kQSeqs];     // INT32_MAX past the last
   int32_t tok[kQSeqs + 1];  // tokens of earlier sequences
   int32_t t0[kQSeqs];
@@ -119,6 +120,7 @@ hipError_t launch_attend_split(const AttendArgs& a, int rt, bool direct, hipStre
 hipError_t launch_attend_join(const AttendArgs& a, int rows, hipStream_t s);
 // Many rows: tiles of kTileRows rows.
 constexpr int kTileRows = 128;
+constexpr int tile_waves(int DP) { return DP <= 128 ? 2 : 1; }  // workgroups a CU
 hipError_t launch_attend_tile(const AttendArgs& a, bool direct, hipStream_t s);
 // Column sums of the probabilities, from the rows' lse.
 constexpr int kWeighTokens = 128;

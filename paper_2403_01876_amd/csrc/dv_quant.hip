@@ -58,9 +58,8 @@ __device__ __forceinline__ float amax_of(const u32x4& a, float m) {
   return m;
 }
 
-constexpr int kHeld = 4;  // units of 16 elements that a lane holds
-
-template <bool BF16>
+// HELD: units that a lane holds.
+template <bool BF16, int HELD>
 __global__ void __launch_bounds__(kThreads) quant_kernel(QuantArgs a) {
   __shared__ int32_t first[kQSeqs];
   for (int i = threadIdx.x; i < a.nseq; i += kThreads) first[i] = a.item[i];
@@ -100,10 +99,10 @@ __global__ void __launch_bounds__(kThreads) quant_kernel(QuantArgs a) {
   const u32x4* src = (const u32x4*)(a.wire + (int64_t)blockIdx.y * a.w_slab +
                                     ((int64_t)a.tok[b] * q.heads + (int64_t)h * n + (lo - t0)) *
                                         q.D * 2);
-  u32x4 x[kHeld][2];
+  u32x4 x[HELD][2];
   float m = 0.f;
 #pragma unroll
-  for (int i = 0; i < kHeld; ++i) {
+  for (int i = 0; i < HELD; ++i) {
     const int u = lane + i * group;
     if (u < units) {
       x[i][0] = __builtin_nontemporal_load(src + 2 * u);
@@ -113,19 +112,19 @@ __global__ void __launch_bounds__(kThreads) quant_kernel(QuantArgs a) {
     }
   }
 #pragma unroll
-  for (int i = 0; i < kHeld; ++i) m = amax_of<BF16>(x[i][0], amax_of<BF16>(x[i][1], m));
-  for (int u = lane + kHeld * group; u < units; u += group)
+  for (int i = 0; i < HELD; ++i) m = amax_of<BF16>(x[i][0], amax_of<BF16>(x[i][1], m));
+  for (int u = lane + HELD * group; u < units; u += group)
     m = amax_of<BF16>(src[2 * u], amax_of<BF16>(src[2 * u + 1], m));
   for (int o = group >> 1; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
   const float p = fmaxf(scale_for(fminf(m, limit<BF16>())), old), inv = inverse(p);
 
   u32x4* dst = (u32x4*)(codes + (int64_t)held * q.D);
 #pragma unroll
-  for (int i = 0; i < kHeld; ++i) {
+  for (int i = 0; i < HELD; ++i) {
     const int u = lane + i * group;
     if (u < units) dst[u] = encode<BF16>(x[i][0], x[i][1], inv);
   }
-  for (int u = lane + kHeld * group; u < units; u += group)
+  for (int u = lane + HELD * group; u < units; u += group)
     dst[u] = encode<BF16>(src[2 * u], src[2 * u + 1], inv);
   if (held && p > old) {  // the codes from before, to the larger scale
     u32x4* was = (u32x4*)codes;
@@ -148,7 +147,11 @@ __global__ void __launch_bounds__(kThreads) quant_kernel(QuantArgs a) {
 }  // namespace
 
 hipError_t launch_quant(const QuantArgs& a, uint32_t nslabs, hipStream_t s) {
-  const void* fn = a.bf16 ? (const void*)&quant_kernel<true> : (const void*)&quant_kernel<false>;
+  const bool few = a.held == 2;
+  const void* fn = a.bf16 ? few ? (const void*)&quant_kernel<true, 2>
+                                : (const void*)&quant_kernel<true, 4>
+                   : few  ? (const void*)&quant_kernel<false, 2>
+                          : (const void*)&quant_kernel<false, 4>;
   const uint32_t per = kThreads >> a.lanes_log2;
   void* args[] = {const_cast<QuantArgs*>(&a)};
   return hipLaunchKernel(fn, dim3(((uint32_t)a.items + per - 1) / per, nslabs), dim3(kThreads),
