@@ -1152,21 +1152,22 @@ __global__ void __launch_bounds__(kThreads) attend_join_kernel(AttendArgs a, int
 }
 
 // ---------------------------------------------------------------------------
-// Weights from many rows: a workgroup takes 128 tokens of a head and every row
-// that may see them; p = exp2(s2 - lse2).  A wave holds 64 tokens' keys and takes
+// Weights from many rows: a workgroup takes 128 tokens of a head and the rows that
+// may see them, or where that leaves the card empty one of several shares of
+// those; p = exp2(s2 - lse2).  A wave holds 64 tokens' keys and takes
 // every other 32 rows, which the workgroup copies to LDS two steps ahead (16-byte
 // pieces stored at piece ^ key(row), as above).  Each sum is one lane's; the
 // lanes', then the two waves', are added in a fixed order.
 // Bound by the exponentials and the product.
 // ---------------------------------------------------------------------------
 template <bool BF16, int DP>
-__global__ void __launch_bounds__(kThreads, DP <= 128 ? 3 : 1) attend_weigh_kernel(AttendArgs a) {
+__global__ void __launch_bounds__(kThreads, weigh_waves(DP)) attend_weigh_kernel(AttendArgs a) {
   using T = Ty<BF16>;
   constexpr int KS = DP / 16, CH = DP / 8;       // products; 16-byte pieces of a row
   constexpr int kStep = 64, kBytes = kStep * DP * 2, kRing = 3;
   constexpr int kLoads = kBytes / 1024 / 4;      // copies of a wave
   __shared__ __attribute__((aligned(1024))) uint8_t rows_of[kRing * kBytes];
-  __shared__ __attribute__((aligned(16))) float words[kRing][4][64];  // rows' lse, slope
+  __shared__ __attribute__((aligned(16))) float words[kRing][2][128];  // rows' lse, slope, position
   __shared__ __attribute__((aligned(16))) float token_at[kWeighTokens];  // positions
   __shared__ float part[2][64];
   const QLayout& q = a.q;
@@ -1210,12 +1211,14 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 3 : 1) attend_weigh_kern
   const int before = len - nq;  // query i sees slots up to before + i
   // the first row that sees the workgroup's first token
   const int from = max(0, t0 - before) * a.G & -kStep;
-  const int steps = rows > from ? (rows - from + kStep - 1) / kStep : 0;
+  const int all = rows > from ? (rows - from + kStep - 1) / kStep : 0;
+  const int shares = gridDim.y, per = scalar((all + shares - 1) / shares);
+  const int k0 = blockIdx.y * per, first = from + k0 * kStep, steps = max(0, min(per, all - k0));
   auto key_of = [](int row) { return CH == 8 ? (row >> 1) & 7 : row & 15; };
   const uint32_t rows_at = scalar(lds_address(rows_of)), words_at = scalar(lds_address(words));
   // (Rows past the last are the last again, and so are steps; both are hidden.)
   auto fetch = [&](int k) {
-    const int r0 = from + min(k, steps - 1) * kStep, slot = k % kRing;
+    const int r0 = first + min(k, steps - 1) * kStep, slot = k % kRing;
     wait_lds();
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
@@ -1230,7 +1233,10 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 3 : 1) attend_weigh_kern
     }
     const int r = min(r0 + odd * 32 + c, rows - 1), qi = a.d_G.div(r), head = h * a.G + r - qi * a.G;
     const float* word = a.row_lse + (int64_t)(seq.tok + qi) * a.q_heads + head;
-    if (a.slopes && hf) word = a.slopes + head;
+    if (a.slopes) {  // the two waves of these rows bring half each
+      if (hf) word = a.slopes + head;
+      if ((wave & 1) && q.position) word = (const float*)(q.position + slots + max(0, before + qi));
+    }
     copy_word_to_lds(word, words_at + (slot * 4 + wave) * 256);
   };
 
@@ -1247,7 +1253,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 3 : 1) attend_weigh_kern
     wait_loads<kLoads + 1>();  // all but the next step's
     lds_barrier();
     fetch(k + 2);
-    const int slot = k % kRing, r0 = from + k * kStep + odd * 32;
+    const int slot = k % kRing, r0 = first + k * kStep + odd * 32;
     const uint8_t* ql = rows_of + slot * kBytes + (odd * 32 + c) * DP * 2;
     const int kk = key_of(c);  // (32 rows on the key is the same)
     f32x16 s[2];
@@ -1262,7 +1268,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 3 : 1) attend_weigh_kern
     }
     settle(s[0]);
     settle(s[1]);
-    const float* w = words[slot][wave];
+    const float* w = words[slot][odd];
     const float lse2 = w[c];
 #pragma unroll
     for (int u = 0; u < 2; ++u)
@@ -1271,7 +1277,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 3 : 1) attend_weigh_kern
     const int limit = r0 + c < rows ? before + (int)a.d_G.div(r0 + c) : -1;
     if (a.slopes) {
       const float slope = w[32 + c] * kLog2e;
-      const float here = limit < 0 ? 0.f : q.position ? (float)q.position[slots + limit] : (float)limit;
+      const float here = q.position ? (float)__float_as_int(w[64 + c]) : (float)limit;
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -1281,14 +1287,16 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 3 : 1) attend_weigh_kern
     // (lse is +infinity for a row that sees nothing: its p are 0, or NaN, and hidden)
     if (before + scalar(r0 / a.G) < tw + 63 || r0 + 32 > rows ||
         (mapped[0] & mapped[1]) != 0xffffffffu) {
+      const int last = lse2 == INFINITY ? -1 : limit - tw - hf * 4;
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int u = 0; u < 2; ++u) {
+        const uint32_t there = mapped[u] >> (hf * 4);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const int o = (i / 4) * 8 + hf * 4 + i % 4;
-          const bool sees = tw + u * 32 + o <= limit && ((mapped[u] >> o) & 1) && lse2 != INFINITY;
-          s[u][i] = sees ? s[u][i] : -INFINITY;
+          const int o = (i / 4) * 8 + i % 4;
+          s[u][i] = u * 32 + o <= last && ((there >> o) & 1) ? s[u][i] : -INFINITY;
         }
+      }
     }
 #pragma unroll
     for (int u = 0; u < 2; ++u)
@@ -1313,9 +1321,29 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 3 : 1) attend_weigh_kern
       if (c == i && tw + o < len) {
         float* to = q.weight + slots + tw + o;
         const float total = sum[u][i] + part[wave & 1][o];
-        *to = a.decay == 0.f ? total : a.decay * *to + total;
+        if (shares > 1)
+          a.sums[((int64_t)blockIdx.y * a.items + item) * kWeighTokens + (tw - t0) + o] = total;
+        else
+          *to = a.decay == 0.f ? total : a.decay * *to + total;
       }
     }
+}
+
+// Adds the shares' sums, in order: a workgroup for the tokens of one above.
+// 5 us, of which 2 are the launch.
+__global__ void __launch_bounds__(kWeighTokens) attend_share_kernel(AttendArgs a, int shares) {
+  const QLayout& q = a.q;
+  const int item = blockIdx.x;
+  const Seq seq = seq_of(a, item);
+  const int tiles = (seq.len + kWeighTokens - 1) / kWeighTokens, h = seq.k / tiles;
+  const int t = (seq.k - h * tiles) * kWeighTokens + threadIdx.x;
+  if (t >= seq.len) return;
+  const float* from = a.sums + (int64_t)item * kWeighTokens + threadIdx.x;
+  float total = 0.f;
+#pragma unroll 8
+  for (int i = 0; i < shares; ++i) total += from[(int64_t)i * a.items * kWeighTokens];
+  float* to = q.weight + (((int64_t)a.layer * q.batch + a.b0 + seq.b) * q.heads + h) * (int64_t)q.cap + t;
+  *to = a.decay == 0.f ? total : a.decay * *to + total;
 }
 
 template <typename... More>
@@ -1373,8 +1401,13 @@ hipError_t launch_attend_join(const AttendArgs& a, int rows, hipStream_t s) {
                 dim3(a.items, std::max(1, rows / 32) + (a.scores ? 1 : 0)), 0, s, a, rows);
 }
 
-hipError_t launch_attend_weigh(const AttendArgs& a, hipStream_t s) {
-  return launch(pick(a, [](auto k) { return decltype(k)::weigh(); }), dim3(a.items), 0, s, a);
+hipError_t launch_attend_weigh(const AttendArgs& a, int shares, hipStream_t s) {
+  const hipError_t e = launch(pick(a, [](auto k) { return decltype(k)::weigh(); }),
+                              dim3(a.items, shares), 0, s, a);
+  if (e != hipSuccess || shares == 1) return e;
+  void* args[] = {const_cast<AttendArgs*>(&a), &shares};
+  return hipLaunchKernel((const void*)&attend_share_kernel, dim3(a.items), dim3(kWeighTokens), args,
+                         0, s);
 }
 
 }  // namespace dv

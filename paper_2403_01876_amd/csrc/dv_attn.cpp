@@ -156,10 +156,18 @@ struct Plan {
   int R;
   int32_t chunk;   // tokens of a split
   int64_t Dp;
-  uint64_t part, ml, scores, lse, bytes;  // bytes of the workspace's parts
+  int64_t most;    // rows of the longest sequence
+  uint64_t part, ml, scores, lse, sums, bytes;  // bytes of the workspace's parts
 };
 
 uint64_t up256(uint64_t n) { return (n + 255) & ~255ull; }
+
+// Shares of the rows that each of `items` work items of the weights is dealt in:
+// as many as the card holds at once, with 256 rows or more.
+int shares_of(const Plan& p, int64_t items) {
+  const int64_t slots = 256 * dv::weigh_waves((int)p.Dp);
+  return (int)std::max<int64_t>(1, std::min(slots / std::max<int64_t>(1, items), p.most / 256));
+}
 
 int64_t splits_of(const Plan& p, int64_t len) {
   return std::max<int64_t>(1, (len + p.chunk - 1) / p.chunk);
@@ -186,6 +194,7 @@ int plan_of(const Quant& q, const int32_t* q_len, const int32_t* kv_len, const d
   // rows are counted in 32 bits
   if (most >= (1ll << 30) || tokens * a->q_heads >= (1ll << 31)) return DV_ERR_UNSUPPORTED;
   p->Dp = dv::padded(v.D);
+  p->most = most;
   p->split = most <= (p->Dp == 256 ? kFewRowsWide : kFewRows);
   if (p->split) {
     p->R = most <= 16 ? 16 : most <= 32 ? 32 : 64;
@@ -234,7 +243,7 @@ int plan_of(const Quant& q, const int32_t* q_len, const int32_t* kv_len, const d
   }
   p->direct = longest <= p->chunk;
   // Workspace of the largest launch; they run one after another.
-  p->part = p->ml = p->scores = p->lse = 0;
+  p->part = p->ml = p->scores = p->lse = p->sums = 0;
   for (int64_t b0 = 0; b0 < v.B; b0 += kQSeqs) {
     uint64_t items = 0, scores = 0, rows = 0;
     int64_t weigh_items = 0;
@@ -253,9 +262,14 @@ int plan_of(const Quant& q, const int32_t* q_len, const int32_t* kv_len, const d
       p->ml = std::max(p->ml, up256(items * p->R * 8));
     }
     if (a->weigh && p->split) p->scores = std::max(p->scores, up256(scores * 128));
-    if (a->weigh && !p->split) p->lse = std::max(p->lse, up256(rows * 4));
+    if (a->weigh && !p->split) {
+      p->lse = std::max(p->lse, up256(rows * 4));
+      const int shares = shares_of(*p, weigh_items);
+      if (shares > 1)
+        p->sums = std::max(p->sums, up256((uint64_t)shares * weigh_items * dv::kWeighTokens * 4));
+    }
   }
-  p->bytes = p->part + p->ml + p->scores + p->lse;
+  p->bytes = p->part + p->ml + p->scores + p->lse + p->sums;
   return DV_OK;
 }
 
@@ -339,6 +353,7 @@ int attend(const dv_quant* c, int32_t mb, int32_t layer, const int32_t* q_len,
   a.ml = reinterpret_cast<float*>(w + p.part);
   a.scores = p.scores ? reinterpret_cast<float*>(w + p.part + p.ml) : nullptr;
   a.row_lse = p.lse ? reinterpret_cast<float*>(w + p.part + p.ml + p.scores) : nullptr;
+  a.sums = reinterpret_cast<float*>(w + p.part + p.ml + p.scores + p.lse);
   a.scale2 = u->scale * 1.4426950408889634f;
   a.decay = u->decay;
   a.layer = layer;
@@ -375,7 +390,7 @@ int attend(const dv_quant* c, int32_t mb, int32_t layer, const int32_t* q_len,
       fill(&a, q_len, kv_len, b0, nseq, G, v.H, [&](int64_t b) {
         return v.H * (((int64_t)kv_len[b] + dv::kWeighTokens - 1) / dv::kWeighTokens);
       });
-      if (a.items) e = dv::launch_attend_weigh(a, st);
+      if (a.items) e = dv::launch_attend_weigh(a, shares_of(p, a.items), st);
     }
     if (e != hipSuccess) return dv::hip_fail(e, "attention launch");
   }

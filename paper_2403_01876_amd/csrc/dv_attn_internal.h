@@ -76,6 +76,7 @@ struct AttendArgs {
   float* ml;
   float* scores;  // weigh, split rows: [sequence][head][row][padded tokens], log2 units
   float* row_lse; // weigh, many rows: [row of the call][q_heads], log2 units
+  float* sums;    // weigh, many rows in shares: [share][item][kWeighTokens]
   float scale2;   // scale * log2 e
   float decay;
   int32_t layer, b0, nseq, items;
@@ -124,7 +125,8 @@ constexpr int tile_waves(int DP) { return DP <= 128 ? 2 : 1; }  // workgroups a 
 hipError_t launch_attend_tile(const AttendArgs& a, bool direct, hipStream_t s);
 // Column sums of the probabilities, from the rows' lse.
 constexpr int kWeighTokens = 128;
-hipError_t launch_attend_weigh(const AttendArgs& a, hipStream_t s);
+constexpr int weigh_waves(int DP) { return DP <= 128 ? 3 : 1; }  // workgroups a CU
+hipError_t launch_attend_weigh(const AttendArgs& a, int shares, hipStream_t s);
 
 // ---- dv_evict ----
 // A work item is a group of `group` blocks of the result of one head of one

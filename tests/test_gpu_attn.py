@@ -231,6 +231,15 @@ def test_attend_long_axis_split(tokens, weights):
     run_attend(c, [tokens, 1], [9000, 4097], 4, "bf16", decay=0.0 if weights else None)
 
 
+@pytest.mark.parametrize("D,tokens", [(64, 700), (128, 333), (256, 130)])
+def test_attend_weights_of_rows_in_shares(D, tokens):
+    """Rows enough for several workgroups to add up each token's weight, some of
+    which see none of its tokens."""
+    c = make("paged", 1, 1, D, 3, 1500, 8, D + 1, companions=True)
+    run_attend(c, [tokens, 1, 90], [1500, 700, 90], 8, "f16" if D == 128 else "bf16",
+               slopes=D != 64, decay=0.25)
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("tokens", [1, 6, 80])
 def test_attend_unmapped_blocks_and_nan(dtype, tokens):
