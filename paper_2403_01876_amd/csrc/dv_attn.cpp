@@ -550,6 +550,9 @@ int dv_evict(const dv_quant* src, int32_t src_mb, const dv_quant* dst, int32_t d
   a.most = (int32_t)longest;
   a.blocks = (int32_t)blocks;
   // Blocks whose tokens are looked up together: 128 tokens, or a block a wave.
+  // (Half of 32 x 128 to 4096 tokens, 8 heads: 64 tokens 78.3 us, 128 78.5, 256
+  // 79.5, 512 89.3, 1024 126; a quarter of 8 x 512 to 1024, 40 heads: 64 and 128
+  // 20, 256 and more 25.)
   a.group = (int32_t)std::max<int64_t>(4, 128 / a.d.bs / 4 * 4);
   a.d_du = dv::fast_div((uint32_t)(v.D / 16));
   hipStream_t st = static_cast<hipStream_t>(stream);

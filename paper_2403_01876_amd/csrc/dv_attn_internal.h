@@ -28,7 +28,7 @@ struct QLayout {
   int64_t c_slab, c_b, c_blk, c_h;
   int32_t bs, D, heads, batch;
   int32_t num_blocks, max_blocks;
-  int32_t cap, pad;
+  int32_t cap;
   FastDiv d_bs;
 };
 
@@ -72,18 +72,18 @@ struct AttendArgs {
   int64_t q_token, q_head, o_token, o_head;  // elements
   const float* slopes;
   float* lse;
-  float* part;    // split rows: [item][RT * 16 rows][Dp] sums, then [item][rows][2] max, sum
-  float* ml;
+  float* part;    // splits: [item][R rows][Dp], sums of a work item's rows
+  float* ml;      // splits: [item][R rows][2], their reference and sum
   float* scores;  // weigh, split rows: [sequence][head][row][padded tokens], log2 units
   float* row_lse; // weigh, many rows: [row of the call][q_heads], log2 units
   float* sums;    // weigh, many rows in shares: [share][item][kWeighTokens]
   float scale2;   // scale * log2 e
   float decay;
   int32_t layer, b0, nseq, items;
-  int32_t G, q_heads, chunk;  // chunk: tokens of a split (rows of a tile where there are many)
+  int32_t G, q_heads, chunk;  // chunk: tokens of a split
   int32_t weigh, bf16, row0;  // row0: rows of q before this launch's
   FastDiv d_G;
-  int32_t nt, pad;            // whether the codes are read past the caches
+  int32_t nt;                 // whether the codes are read past the caches
   int32_t item[kQSeqs];       // work items of earlier sequences; INT32_MAX past the last
   int32_t tok[kQSeqs + 1];    // queries of earlier sequences
   int32_t len[kQSeqs];        // tokens in the cache
@@ -97,7 +97,7 @@ inline int padded(int64_t D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 // Tokens of a wave's step over the cache, and of a workgroup's (four waves).
 constexpr int kSplitStep = 32;
 constexpr int kSplitRound = 4 * kSplitStep;
-constexpr int kSplitChunkMax = 1792;
+constexpr int kSplitChunkMax = 1792;  // its tables take 28 KB of LDS at most
 // Bytes of LDS for the queries of the split kernel: those of four tiles leave no
 // registers for two workgroups a CU.
 constexpr int split_queries(int DP, int RT) { return RT == 4 ? RT * DP * 32 : 0; }
@@ -136,7 +136,7 @@ struct EvictArgs {
   int32_t* kept;
   int32_t kept_stride, recent, l0, nl;
   int32_t b0, nseq, in_place, most;  // most: tokens of the longest sequence
-  int32_t blocks, group, items, pad;  // blocks: most result blocks of a sequence
+  int32_t blocks, group, items;  // blocks: most result blocks of a sequence
   FastDiv d_du;                       // by 16-code units of a token
   int32_t len[kQSeqs];
   int32_t keep[kQSeqs];

