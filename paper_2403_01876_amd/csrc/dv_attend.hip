@@ -561,8 +561,9 @@ __global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
   // The scales follow the first codes: both are on their way at once.
   for (int i = tid; i < ((cn + kSplitStep - 1) & -kSplitStep); i += kThreads) {
     const int blk = ((const int*)ks)[i];
+    // (a probability of 0 times a scale that nothing wrote may be NaN)
     ks[i] = blk < 0 ? NAN : sk[blk * q.c_blk] * a.scale2;
-    vs[i] = sk[max(blk, 0) * q.c_blk + q.c_slab];
+    vs[i] = blk < 0 ? 0.f : sk[blk * q.c_blk + q.c_slab];
   }
   lds_barrier();
   for (; t < cn; t += kSplitRound) step(t, t + kSplitRound < cn);
@@ -831,6 +832,7 @@ __global__ void __launch_bounds__(kThreads, tile_waves(DP))
     uint8_t* to = lds + (half ? L::kValues + (n & 1) * L::vBuf : L::kKeys + (n & 1) * L::kBuf) +
                   tok * (half ? vPitch : kPitch) + p * 32;
     if (y.entry < 0 || p * 16 >= q.D) y.x = u32x4{0, 0, 0, 0};  // not there
+    if (y.entry < 0) y.scale = 1.f;  // (0 times a scale that nothing wrote may be NaN)
     // Values that some row does not see: NaN becomes 0 (spread_nan).
     if (half && (begin + (n + 1) * kTile - 1 > all_see || holes)) {
       uint32_t nan = 0;
