@@ -242,10 +242,10 @@ __global__ void __launch_bounds__(kThreads) evict_move_kernel(EvictArgs a) {
       const int t = kept[j0 * d.bs + i], sj = s.d_bs.div(t);
       int64_t blk = s.bt ? s.bt[(int64_t)sb * s.max_blocks + sj] : sj;
       const bool hole = s.bt && (uint64_t)blk >= (uint64_t)s.num_blocks;
-      blk = hole ? 0 : blk;
       table[i] = hole ? ~0u : (uint32_t)((blk * s.s_blk + (int64_t)(t - sj * s.bs) * s.D) >> 4);
-      scales[i] = from_scale[blk * s.c_blk];
-      scales[span + i] = from_scale[blk * s.c_blk + s.c_slab];
+      // (zeros times another block's scale, which nothing may have written, may be NaN)
+      scales[i] = hole ? 1.f : from_scale[blk * s.c_blk];
+      scales[span + i] = hole ? 1.f : from_scale[blk * s.c_blk + s.c_slab];
     }
     __syncthreads();
     // jobs: blocks j0 + wave + 4 x, keys then values
