@@ -117,7 +117,10 @@ DV_API int dv_attend_bytes(const dv_quant* c, const int32_t* q_len, const int32_
  * (with decay 0 the old weight is not read); sequences without queries keep
  * their weights.  Codes past a query's slot do not enter its result, NaN or
  * not; slots in unmapped blocks are not seen.  Scores, sums and weights are kept
- * in 32 bits; a cached number beyond f16 is infinite to queries in f16.
+ * in 32 bits.  Where a sequence of the call has more than 64 rows (q_len times G;
+ * 32 for head_dim above 128), cached numbers are read in the queries' type: f16
+ * takes those beyond it (of a cache rounded from bf16) as its largest and those
+ * of the smallest magnitudes to a multiple of 2^-24.
  * head_dim at most 256 (DV_ERR_UNSUPPORTED); one layer's keys at most 64 GB.
  * Results do not depend on the order in which workgroups run.  q, the cache and
  * its table are not written; out, lse, workspace and weights must not overlap

@@ -50,6 +50,14 @@ struct Ty<false> {
   static __device__ __forceinline__ uint32_t cvt(uint32_t w, float s) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, s, HI));
   }
+  // What f16 does not hold (a cache rounded from bf16) becomes its largest number: an
+  // infinity would be NaN to every row that gives it a probability of 0, hidden
+  // or not.  The largest scale whose products with all codes f16 holds, and two
+  // converted numbers made finite:
+  static constexpr float kHeld = 128.f;
+  static __device__ __forceinline__ uint32_t finite(uint32_t w) {
+    return w - ((w & 0x7fffu) == 0x7c00u) - ((uint32_t)((w & 0x7fff0000u) == 0x7c000000u) << 16);
+  }
   static __device__ __forceinline__ uint32_t pack(float a, float b) {
     return __builtin_bit_cast(uint32_t, f16x2{(_Float16)a, (_Float16)b});
   }
@@ -75,6 +83,8 @@ struct Ty<true> {
   static __device__ __forceinline__ uint32_t cvt(uint32_t w, float s) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, HI));
   }
+  static constexpr float kHeld = INFINITY;  // (bf16 holds what f32 does)
+  static __device__ __forceinline__ uint32_t finite(uint32_t w) { return w; }
   static __device__ __forceinline__ uint32_t pack(float a, float b) {
     return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
   }
@@ -847,12 +857,19 @@ __global__ void __launch_bounds__(kThreads, tile_waves(DP))
         nan_to = n + 1;
       }
     }
+    u32x4 x[2];
 #pragma unroll
     for (int e = 0; e < 2; ++e)
-      *(u32x4*)(to + e * 16) = u32x4{
+      x[e] = u32x4{
           T::template cvt<false>(y.x[2 * e], y.scale), T::template cvt<true>(y.x[2 * e], y.scale),
           T::template cvt<false>(y.x[2 * e + 1], y.scale),
           T::template cvt<true>(y.x[2 * e + 1], y.scale)};
+    if (y.scale > T::kHeld) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i / 4][i % 4] = T::finite(x[i / 4][i % 4]);
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e) *(u32x4*)(to + e * 16) = x[e];
   };
 
   f32x16 o[DB], s;
@@ -1211,6 +1228,8 @@ __global__ void __launch_bounds__(kThreads, weigh_waves(DP)) attend_weigh_kernel
       if (d < q.D) w = *(const u32x2*)(p + d);
       kr[u][s] = u32x4{T::template cvt<false>(w[0], scale), T::template cvt<true>(w[0], scale),
                        T::template cvt<false>(w[1], scale), T::template cvt<true>(w[1], scale)};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) kr[u][s][i] = T::finite(kr[u][s][i]);
     }
   }
   if (a.slopes && tid < kWeighTokens) {

@@ -59,3 +59,62 @@ def test_evict_unwritten_scales_of_unowned_blocks(scale, D, bs, place):
     assert np.array_equal(td["scale"].cpu().numpy(), d.scale, equal_nan=True)
     got = td["codes"].cpu().numpy()
     assert ref.same_codes(got, d.codes), f"{int((got != d.codes).sum())} codes differ"
+
+
+# ---- numbers that a 16-bit type does not hold -----------------------------------------------
+
+
+class Saturated(ref.Cache8):
+    """What queries in f16 make of a cache where a call rounds what it reads."""
+
+    def values(self, l, kv, b, h, n):
+        x, ok = super().values(l, kv, b, h, n)
+        return np.clip(x, -65504.0, 65504.0), ok
+
+
+@pytest.mark.parametrize("D,group,tokens", [(64, 2, 150), (128, 8, 40), (256, 1, 70)])
+def test_attend_values_beyond_f16(D, group, tokens):
+    """Hidden from a row they do not touch it; seen, they count as f16's largest."""
+    rng = np.random.default_rng(D)
+    c = Saturated("dense", 1, 2, D, 2, 300, 16, rng, companions=True)
+    c.scale[0, 1, :, :, 18] = 2.0 ** 12  # values of slots 288 to 299
+    c.scale[0, 1, 0, 1, 17] = 2.0 ** 60
+    y = run_attend(c, [tokens, 9], [300, 300], group, "f16", decay=0.0)
+    assert np.isfinite(y).all() and np.abs(y).max() > 1000
+
+
+@pytest.mark.parametrize("D,group,tokens", [(64, 2, 150), (128, 8, 40), (256, 1, 70)])
+def test_attend_keys_beyond_f16(D, group, tokens):
+    rng = np.random.default_rng(D)
+    c = Saturated("paged", 1, 2, D, 2, 300, 16, rng, companions=True)
+    for j in (3, 18):
+        c.scale[0, 0, c.table[0, j]] = 2.0 ** 12
+    c.scale[0, 0, c.table[1, 18], 0] = 2.0 ** 100
+    y = run_attend(c, [tokens, 9], [300, 300], group, "f16", decay=0.0, spread=2.0 ** -14)
+    assert np.isfinite(y).all()
+
+
+@pytest.mark.parametrize("tokens", [1, 70])
+def test_attend_far_scales(tokens):
+    """bf16 holds every number of a cache rounded from it."""
+    c = make("paged", 1, 2, 64, 2, 200, 8, 5, companions=True)
+    c.scale[0, 0] *= 2.0 ** -54
+    c.scale[0, 1] *= 2.0 ** 100
+    run_attend(c, [tokens, 1], [200, 77], 2, "bf16", decay=0.0, spread=2.0 ** 53)
+
+
+@pytest.mark.parametrize("tokens", [1, 70])
+def test_attend_numbers_below_the_normal_ones_of_f16(tokens):
+    """Keys and values that are multiples of 2^-24, as rounded from f16's smallest."""
+    rng = np.random.default_rng(6)
+    c = make("dense", 1, 2, 64, 2, 200, 8, 6, companions=True)
+    c.codes = ref.encode(np.round(rng.normal(size=c.codes.shape) * 6).clip(-28, 28) * 16)
+    c.scale[...] = 2.0 ** -28
+    run_attend(c, [tokens, 1], [200, 77], 2, "f16", decay=0.0, spread=2.0 ** 12)
+
+
+def test_attend_few_rows_keep_numbers_beyond_f16():
+    c = make("dense", 1, 2, 64, 2, 300, 16, 7, companions=True)
+    c.scale[0, 0, :, :, 3] = 2.0 ** 12
+    c.scale[0, 1, :, :, 4] = 2.0 ** 9
+    run_attend(c, [1, 1], [300, 211], 2, "f16", decay=0.0, spread=2.0 ** -16)
