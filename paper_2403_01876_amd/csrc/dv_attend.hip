@@ -131,6 +131,16 @@ __device__ __forceinline__ Seq seq_of(const AttendArgs& a, int item) {
   return q;
 }
 
+// Positions as numbers in 32 bits: less the last token's, so that distances are exact
+// up to 2^24 tokens back, however late in a text they stand.  (Slots are at most 2^24.)
+__device__ __forceinline__ int last_position(const QLayout& q, const float* slopes, int64_t slots,
+                                             int len) {
+  return slopes && q.position && len > 0 ? q.position[slots + len - 1] : 0;
+}
+__device__ __forceinline__ float from_last(int position, int last) {
+  return (float)(int)((uint32_t)position - (uint32_t)last);
+}
+
 // A value known to be the same in all lanes, as a scalar (quotients are not seen to be).
 __device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
@@ -322,6 +332,7 @@ __global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
   const uint8_t* vb = kb + q.s_slab;
   const float* sk = q.scale + slab * q.c_slab + sb * q.c_b + h * q.c_h;
   const int64_t slots = (((int64_t)a.layer * q.batch + sb) * q.heads + h) * (int64_t)q.cap;
+  const int last_at = last_position(q, a.slopes, slots, len);
   int bad = 0;
   for (int i = tid; i < ((cn + kSplitStep - 1) & -kSplitStep); i += kThreads) {
     const int t = min(c0 + i, len - 1), j = q.d_bs.div(t);
@@ -334,7 +345,7 @@ __global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
     }
     off[i] = (uint32_t)((blk * q.s_blk + (int64_t)(t - j * q.bs) * q.D) >> 4);
     ((int*)ks)[i] = hole ? -1 : (int)blk;
-    if (a.slopes) pos[i] = (float)(q.position ? q.position[slots + t] : t);
+    if (a.slopes) pos[i] = q.position ? from_last(q.position[slots + t], last_at) : (float)t;
     bad |= hole;
   }
 
@@ -360,7 +371,7 @@ __global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
       float slope = 0.f, here = 0.f;
       if (a.slopes && limit >= 0) {
         slope = a.slopes[head] * kLog2e;
-        here = (float)(q.position ? q.position[slots + limit] : limit);
+        here = q.position ? from_last(q.position[slots + limit], last_at) : (float)limit;
       }
       columns[r] = f32x4{__int_as_float(limit), slope, here, 0.f};
     }
@@ -761,9 +772,10 @@ __global__ void __launch_bounds__(kThreads, tile_waves(DP))
   // (A factor of 0 makes equal scores; as a tiny one it leaves hidden ones at -infinity.)
   const float factor = fmaxf(fabsf(a.scale2), 0x1p-126f);
   float slope = 0.f, here = 0.f;
+  const int last_at = last_position(q, a.slopes, slots, len);
   if (a.slopes && limit >= 0) {
     slope = a.slopes[head] * kLog2e;
-    here = (float)(q.position ? q.position[slots + limit] : limit);
+    here = q.position ? from_last(q.position[slots + limit], last_at) : (float)limit;
   }
 
   // ---- segments: thread tid stands for token begin + 256 g + tid ----
@@ -886,7 +898,8 @@ __global__ void __launch_bounds__(kThreads, tile_waves(DP))
     const int slot = slot_of(0), blk = place(0, bt ? bt[q.d_bs.div(slot)] : 0);
     table(0, kKeyScale)[tid] = sk[blk * q.c_blk];
     table(0, kValueScale)[tid] = sk[blk * q.c_blk + q.c_slab];
-    if (a.slopes && q.position) ((int*)table(0, kPosition))[tid] = q.position[slots + slot];
+    if (a.slopes && q.position)
+      table(0, kPosition)[tid] = from_last(q.position[slots + slot], last_at);
     __syncthreads();
     holes = any_hole(0);
     for (int n = 0; n < kAhead; ++n) fetch(n, N - 1);
@@ -910,7 +923,13 @@ __global__ void __launch_bounds__(kThreads, tile_waves(DP))
     // waits below have let what was asked for two steps ago arrive.
     if (n % kPerSegment == 0 && n > 0) holes = next_holes;
     if ((g + 1) * kPerSegment < N) {
-      if (n % kPerSegment == 4) next_holes = any_hole(g + 1);
+      if (n % kPerSegment == 4) {
+        next_holes = any_hole(g + 1);
+        if (a.slopes && q.position) {  // what this lane asked for
+          float* x = table(g + 1, kPosition) + tid;
+          *x = from_last(*(const int*)x, last_at);
+        }
+      }
       if (n % kPerSegment == 0 && bt)
         copy_word_to_lds(bt + q.d_bs.div(slot_of(g + 1)),
                          scalar(lds_address(table(g + 1, kEntry) + wave * 64)));
@@ -936,10 +955,7 @@ __global__ void __launch_bounds__(kThreads, tile_waves(DP))
       mul = 1.f;
       const float* at = table(g, kPosition) + n % kPerSegment * kTile + hf * 4;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float x = at[(i / 4) * 8 + i % 4];
-        s[i] = s[i] * factor + slope * ((q.position ? (float)__float_as_int(x) : x) - here);
-      }
+      for (int i = 0; i < 16; ++i) s[i] = s[i] * factor + slope * (at[(i / 4) * 8 + i % 4] - here);
     }
     const bool mask = holes || t + kTile - 1 > all_see;
     if (mask) {
@@ -1232,9 +1248,10 @@ __global__ void __launch_bounds__(kThreads, weigh_waves(DP)) attend_weigh_kernel
       for (int i = 0; i < 4; ++i) kr[u][s][i] = T::finite(kr[u][s][i]);
     }
   }
+  const int last_at = last_position(q, a.slopes, slots, len);
   if (a.slopes && tid < kWeighTokens) {
     const int x = min(t0 + tid, len - 1);
-    token_at[tid] = (float)(q.position ? q.position[slots + x] : x);
+    token_at[tid] = q.position ? from_last(q.position[slots + x], last_at) : (float)x;
   }
 
   const int before = len - nq;  // query i sees slots up to before + i
@@ -1306,7 +1323,7 @@ __global__ void __launch_bounds__(kThreads, weigh_waves(DP)) attend_weigh_kernel
     const int limit = r0 + c < rows ? before + (int)a.d_G.div(r0 + c) : -1;
     if (a.slopes) {
       const float slope = w[32 + c] * kLog2e;
-      const float here = q.position ? (float)__float_as_int(w[64 + c]) : (float)limit;
+      const float here = q.position ? from_last(__float_as_int(w[64 + c]), last_at) : (float)limit;
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll

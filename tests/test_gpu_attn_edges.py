@@ -118,3 +118,15 @@ def test_attend_few_rows_keep_numbers_beyond_f16():
     c.scale[0, 0, :, :, 3] = 2.0 ** 12
     c.scale[0, 1, :, :, 4] = 2.0 ** 9
     run_attend(c, [1, 1], [300, 211], 2, "f16", decay=0.0, spread=2.0 ** -16)
+
+
+# ---- positions past 2^24, scores past 1e30 ---------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("tokens", [1, 90])
+@pytest.mark.parametrize("first", [2 ** 25 - 300, 2 ** 31 - 2000])
+def test_attend_distances_of_late_positions(dtype, tokens, first):
+    c = make("dense", 1, 2, 64, 2, 300, 16, 8, companions=True)
+    c.position += np.int32(first)
+    run_attend(c, [tokens, 3], [300, 41], 2, dtype, slopes=True, decay=0.0)
