@@ -34,7 +34,8 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-constexpr float kLow = -1e30f;  // "no score yet"; a hidden score is -infinity
+// "No score yet", the lowest number; a hidden score is -infinity.
+constexpr float kLow = -3.402823466e38f;
 constexpr float kLn2 = 0.69314718055994531f, kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 8.f;
 
@@ -890,6 +891,7 @@ __global__ void __launch_bounds__(kThreads, tile_waves(DP))
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
   float m = kLow, sum = 0.f;
+  bool scaled = a.slopes != nullptr;  // whether scores get their factor by themselves
   auto key = [&](int n, int e) {
     return *(const u32x4*)(lds + L::kKeys + (n & 1) * L::kBuf + c * kPitch + e * 32 + hf * 16);
   };
@@ -951,11 +953,15 @@ __global__ void __launch_bounds__(kThreads, tile_waves(DP))
 
     // This tile's scores: bias, what is hidden, the reference.
     float mul = factor;
-    if (a.slopes) {
+    if (scaled) {
       mul = 1.f;
-      const float* at = table(g, kPosition) + n % kPerSegment * kTile + hf * 4;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = s[i] * factor + slope * (at[(i / 4) * 8 + i % 4] - here);
+      for (int i = 0; i < 16; ++i) s[i] *= factor;
+      if (a.slopes) {
+        const float* at = table(g, kPosition) + n % kPerSegment * kTile + hf * 4;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] += slope * (at[(i / 4) * 8 + i % 4] - here);
+      }
     }
     const bool mask = holes || t + kTile - 1 > all_see;
     if (mask) {
@@ -979,6 +985,14 @@ __global__ void __launch_bounds__(kThreads, tile_waves(DP))
       sum *= f;
 #pragma unroll
       for (int d = 0; d < DB; ++d) o[d] = o[d] * f;
+      // The reference is a rounded score; scores this large pass it by powers of two
+      // that the types do not hold unless they are rounded first too.
+      if (!scaled && __any(fabsf(m) > 0x1p22f && m > kLow)) {
+        scaled = true;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] *= mul;
+        mul = 1.f;
+      }
     }
     const uint8_t* vt = lds + L::kValues + (n & 1) * L::vBuf + (hf * 4 + ((l & 15) >> 2)) * vPitch + ((l >> 4) & 1) * 32 +
                         (l & 3) * 8;

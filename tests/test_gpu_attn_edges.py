@@ -8,7 +8,7 @@ import torch
 
 from paper_2403_01876_amd import attn, dv
 from tests import attn_ref as ref
-from tests.test_gpu_attn import make, run_attend, tie_weights
+from tests.test_gpu_attn import HALF, PROB, make, run_attend, tie_weights
 
 pytestmark = pytest.mark.gpu
 
@@ -130,3 +130,23 @@ def test_attend_distances_of_late_positions(dtype, tokens, first):
     c = make("dense", 1, 2, 64, 2, 300, 16, 8, companions=True)
     c.position += np.int32(first)
     run_attend(c, [tokens, 3], [300, 41], 2, dtype, slopes=True, decay=0.0)
+
+
+@pytest.mark.parametrize("tokens,length", [(1, 200), (1, 3000), (70, 200), (70, 3000)])
+def test_attend_scores_below_minus_1e30(tokens, length):
+    """Equal scores of about -1e32: the mean of the values."""
+    c = make("dense", 1, 1, 64, 1, length, 16, 9)
+    c.codes[0, 0] = 126
+    c.scale[0, 0] = 2.0 ** 100
+    d, _ = c.device(dv, attn)
+    q = torch.full((tokens, 1, 64), -2.0 ** -3, dtype=torch.bfloat16, device="cuda")
+    out, lse = torch.empty_like(q), torch.empty((tokens, 1), device="cuda")
+    nb = attn.dv_attend_bytes(d, [tokens], [length], q)
+    ws = torch.empty(nb, dtype=torch.uint8, device="cuda")
+    attn.dv_attend(d, 0, 0, [tokens], [length], q, out, 0.125, lse=lse, workspace=ws)
+    want, mass, wlse, _ = ref.attend(c, 0, [tokens], [length], q.double().cpu().numpy(), 0.125)
+    many = tokens > 64
+    tol = HALF["bf16"] * np.abs(want) + (PROB + (HALF["bf16"] if many else 0)) * mass + 2.0 ** -24
+    assert np.all(np.abs(out.double().cpu().numpy() - want) <= tol)
+    assert np.all(wlse < -1e31)
+    assert np.all(np.abs(lse.double().cpu().numpy() - wlse) <= 1e-5 * np.abs(wlse))
