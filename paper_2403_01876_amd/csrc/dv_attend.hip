@@ -877,7 +877,7 @@ __global__ void __launch_bounds__(kThreads, tile_waves(DP))
           T::template cvt<false>(y.x[2 * e], y.scale), T::template cvt<true>(y.x[2 * e], y.scale),
           T::template cvt<false>(y.x[2 * e + 1], y.scale),
           T::template cvt<true>(y.x[2 * e + 1], y.scale)};
-    if (y.scale > T::kHeld) {
+    if (__any(y.scale > T::kHeld)) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i / 4][i % 4] = T::finite(x[i / 4][i % 4]);
     }
