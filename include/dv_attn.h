@@ -141,9 +141,9 @@ DV_API int dv_attend(const dv_quant* c, int32_t mb, int32_t layer, const int32_t
  * ascending; entries past a sequence's count are left as they are.
  * `src` needs its weight array.  `dst` may be `src` itself (the same microbatch
  * of the same arrays and layout: compaction in place) or another cache of the
- * same layers, heads, head_dim and batch, disjoint from it.  Slots that an
- * unmapped block leaves without codes count as zeros; blocks that `dst` does not
- * map are skipped.
+ * same layers, heads, head_dim and batch, disjoint from it (one block table may
+ * serve both).  Slots that an unmapped block leaves without codes count as zeros;
+ * blocks that `dst` does not map are skipped.
  * DV_OK, DV_ERR_INVALID, DV_ERR_RANGE, DV_ERR_UNSUPPORTED, DV_ERR_HIP. */
 DV_API int dv_evict(const dv_quant* src, int32_t src_mb, const dv_quant* dst, int32_t dst_mb,
                     int32_t l0, int32_t l1, const int32_t* len, const int32_t* keep,

@@ -68,20 +68,24 @@ int quant_of(const dv_quant* c, int32_t mb, Quant* q) {
 
 uint64_t held(const void* p, uint64_t n) { return p ? n : 0; }
 
-// Whether [p, p + n) overlaps anything of the cache.
-bool hits(const Quant& q, const void* p, uint64_t n) {
-  return overlaps(p, n, q.v.base, q.v.bytes) || dv::overlaps_table(q.v, p, n) ||
-         overlaps(p, n, q.scale, q.scale_bytes) ||
+// Whether [p, p + n) overlaps anything of the cache but its table.
+bool hits_arrays(const Quant& q, const void* p, uint64_t n) {
+  return overlaps(p, n, q.v.base, q.v.bytes) || overlaps(p, n, q.scale, q.scale_bytes) ||
          overlaps(p, n, q.weight, held(q.weight, q.slot_bytes)) ||
          overlaps(p, n, q.position, held(q.position, q.slot_bytes));
 }
 
-// The same of two caches.
+// Whether [p, p + n) overlaps anything of the cache.
+bool hits(const Quant& q, const void* p, uint64_t n) {
+  return hits_arrays(q, p, n) || dv::overlaps_table(q.v, p, n);
+}
+
+// Whether two caches overlap, other than by tables, which calls only read.
 bool hits(const Quant& a, const Quant& b) {
   return hits(a, b.v.base, b.v.bytes) || hits(a, b.scale, b.scale_bytes) ||
          hits(a, b.weight, held(b.weight, b.slot_bytes)) ||
          hits(a, b.position, held(b.position, b.slot_bytes)) ||
-         (b.v.bt && hits(a, b.v.bt, (uint64_t)b.v.B * b.v.max_blocks * 4));
+         (b.v.bt && hits_arrays(a, b.v.bt, (uint64_t)b.v.B * b.v.max_blocks * 4));
 }
 
 // A cache whose own parts overlap.

@@ -150,3 +150,26 @@ def test_attend_scores_below_minus_1e30(tokens, length):
     assert np.all(np.abs(out.double().cpu().numpy() - want) <= tol)
     assert np.all(wlse < -1e31)
     assert np.all(np.abs(lse.double().cpu().numpy() - wlse) <= 1e-5 * np.abs(wlse))
+
+
+# ---- tables, sizes --------------------------------------------------------------------------
+
+
+def test_evict_between_pools_of_one_table():
+    """Two pools that one block table serves: both only read it."""
+    rng = np.random.default_rng(13)
+    c = make("paged", 1, 2, 32, 2, 64, 8, 14, companions=True)
+    d = make("paged", 1, 2, 32, 2, 64, 8, 15, companions=True)
+    d.table = c.table
+    tie_weights(c, rng)
+    (qc, tc), (_, td) = c.device(dv, attn), d.device(dv, attn)
+    qd = attn.QuantCache(
+        dv.Cache(dv.DV_PAGED, 1, 2, 32, 2, [td["codes"]], elem_bytes=1, block_size=8,
+                 num_blocks=d.nblocks, max_blocks=d.mb, block_tables=[tc["table"]]),
+        [td["scale"]], weights=[td["weight"]], positions=[td["position"]])
+    kept = torch.full((1, 2, 2, 30), -1, dtype=torch.int32, device="cuda")
+    attn.dv_evict(qc, 0, qd, 0, 0, 1, [64, 50], [30, 25], 4, kept)
+    want = ref.evict(c, d, 0, 1, [64, 50], [30, 25], 4, 30)
+    assert np.array_equal(kept.cpu().numpy(), want)
+    assert np.array_equal(td["scale"].cpu().numpy(), d.scale)
+    assert ref.same_codes(td["codes"].cpu().numpy(), d.codes)
