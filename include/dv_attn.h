@@ -81,7 +81,7 @@ DV_API int dv_quant_in(const dv_quant* dst, int32_t mb, int32_t l0, int32_t l1, 
 /* Queries and results of dv_attend.  Token i of sequence b is row
  * sum_{b' < b} q_len[b'] + i of q and out; element d of its head g lies at
  * row * token stride + g * head stride + d (strides in elements, multiples of 8
- * below 2^31; bases 16-byte aligned). */
+ * below 2^31; bases 16-byte aligned).  No two rows of out share an element. */
 typedef struct dv_attend_args {
   int32_t type;     /* dv_type of q and out */
   int32_t q_heads;  /* a multiple of the cache's heads: query heads [k*G, (k+1)*G) share

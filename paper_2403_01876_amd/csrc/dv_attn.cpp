@@ -277,6 +277,21 @@ int plan_of(const Quant& q, const int32_t* q_len, const int32_t* kv_len, const d
   return DV_OK;
 }
 
+// Whether two of n * m rows of D elements share one: row (i, j) starts at i * s + j * t.
+bool collide(int64_t n, int64_t s, int64_t m, int64_t t, int64_t D) {
+  if ((n > 1 && s < D) || (m > 1 && t < D)) return true;
+  if (n == 1 || m == 1 || (m - 1) * t + D <= s || (n - 1) * s + D <= t) return false;
+  // Two rows lie |i * s - j * t| apart, i below n and j below m: for each j the
+  // nearest i on either side.
+  for (int64_t j = 1; j < m; ++j) {
+    const int64_t i = j * t / s, over = j * t - i * s;
+    if (i < n && over < D) return true;
+    if (i + 1 < n && s - over < D) return true;
+    if (i >= n) return false;  // and farther for every later j
+  }
+  return false;
+}
+
 // Sequences [b0, b0 + nseq) of a launch, `items(b)` work items each.
 template <typename Items>
 void fill(dv::AttendArgs* a, const int32_t* q_len, const int32_t* kv_len, int64_t b0, int nseq,
@@ -320,8 +335,7 @@ int attend(const dv_quant* c, int32_t mb, int32_t layer, const int32_t* q_len,
       !aligned4(u->lse) || !aligned16(u->workspace))
     return DV_ERR_INVALID;
   // rows of the result must not lie on each other
-  if (u->q_heads > 1 && u->out_head < D) return DV_ERR_INVALID;
-  if (tokens > 1 && u->out_token < D) return DV_ERR_INVALID;
+  if (collide(tokens, u->out_token, u->q_heads, u->out_head, D)) return DV_ERR_INVALID;
   if (u->workspace_bytes < p.bytes) return DV_ERR_SPACE;
   if (p.bytes && !u->workspace) return DV_ERR_INVALID;
   if (tangled(q)) return DV_ERR_INVALID;

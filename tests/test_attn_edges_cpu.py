@@ -1,9 +1,11 @@
 """Refusals of the 8-bit cache operators that go by more than one argument, without a
 GPU: what is refused and what is not is told apart by a later refusal."""
 import numpy as np
+import pytest
 
 from paper_2403_01876_amd import attn, dv
-from tests.test_attn_cpu import (FAKE, INVALID, KEPT, POS, SCALE, TABLE, UNSUPPORTED, WEIGHT)
+from tests.test_attn_cpu import (FAKE, INVALID, KEPT, POS, SCALE, SPACE, TABLE, UNSUPPORTED, WEIGHT,
+                                 attend, cache)
 
 
 def pool(at, table, blocks=128, heads=1 << 16):
@@ -30,3 +32,21 @@ def test_evict_between_pools_of_one_table():
         assert evict(src, pool(1 << 45, at + 64)) == INVALID
         assert evict(pool(0, at + (1 << 45) + 64), pool(1 << 45, TABLE)) == INVALID
     assert evict(src, pool(0, TABLE + 4096)) == INVALID  # one pool, two tables
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_attend_rows_of_the_result_that_share_elements(seed):
+    """Refused exactly where two rows do, whichever of the strides is the larger."""
+    r = np.random.default_rng(seed)
+    D, c = 64, cache(S=64)
+    seen = set()
+    for _ in range(60):
+        tokens, heads = int(r.integers(1, 7)), 2 * int(r.integers(1, 5))
+        token, head = (8 * int(r.choice([r.integers(0, 9), r.integers(8, 90)])) for _ in range(2))
+        starts = np.sort((np.arange(tokens)[:, None] * token + np.arange(heads) * head).ravel())
+        shared = bool((np.diff(starts) < D).any())
+        got = attend(c, q_len=(tokens, 0, 0), kv_len=(9, 0, 0), q_heads=heads, rows=tokens,
+                     q_token=heads * D, out_token=token, out_head=head, weigh=1, workspace_bytes=0)
+        assert got == (INVALID if shared else SPACE), (tokens, heads, token, head)
+        seen.add((shared, token < head))
+    assert len(seen) == 4
