@@ -277,11 +277,11 @@ __device__ __forceinline__ void copy_to_lds(const uint8_t* from, uint32_t lds) {
   if constexpr (NT)
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt"
                  ::"v"(from), "s"(lds)
-                 : "memory");
+                 : "memory", "m0");
   else
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
                  ::"v"(from), "s"(lds)
-                 : "memory");
+                 : "memory", "m0");
 }
 // Waits until at most N of this wave's accesses to memory are on their way.
 template <int N>
@@ -695,7 +695,7 @@ constexpr int kTile = 32, kSegment = 256, kPerSegment = kSegment / kTile, kAhead
 __device__ __forceinline__ void copy_word_to_lds(const void* from, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off"
                ::"v"(from), "s"(lds)
-               : "memory");
+               : "memory", "m0");
 }
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)p;

@@ -1,11 +1,14 @@
 """Refusals of the 8-bit cache operators that go by more than one argument, without a
 GPU: what is refused and what is not is told apart by a later refusal."""
+import os
+import re
+
 import numpy as np
 import pytest
 
 from paper_2403_01876_amd import attn, dv
 from tests.test_attn_cpu import (FAKE, INVALID, KEPT, POS, SCALE, SPACE, TABLE, UNSUPPORTED, WEIGHT,
-                                 attend, cache)
+                                 ROOT, attend, cache)
 
 
 def pool(at, table, blocks=128, heads=1 << 16):
@@ -50,3 +53,13 @@ def test_attend_rows_of_the_result_that_share_elements(seed):
         assert got == (INVALID if shared else SPACE), (tokens, heads, token, head)
         seen.add((shared, token < head))
     assert len(seen) == 4
+
+
+def test_inline_assembly_names_the_registers_it_writes():
+    """A copy to LDS sets m0, which the compiler may use for itself."""
+    text = open(os.path.join(ROOT, "paper_2403_01876_amd", "csrc", "dv_attend.hip")).read()
+    blocks = re.findall(r"asm volatile\((.*?)\);", text, re.S)
+    writes = [b for b in blocks if re.search(r"\bm0,", b)]
+    assert len(writes) == 3
+    for b in writes:
+        assert re.search(r':[^:]*"m0"[^:]*$', b), b
