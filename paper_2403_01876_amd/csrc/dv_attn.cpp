@@ -555,8 +555,10 @@ int dv_evict(const dv_quant* src, int32_t src_mb, const dv_quant* dst, int32_t d
     return DV_ERR_INVALID;
   const int64_t blocks = (most + d.sb - 1) / d.sb;
   if (v.H * blocks >= kMaxItems) return DV_ERR_UNSUPPORTED;
-  // sequences of a launch: its grid's width is theirs times heads times blocks
-  const int64_t seqs = std::min<int64_t>(kQSeqs, kMaxItems / (v.H * blocks));
+  // Sequences of a launch: its grids' widths are theirs times heads, times blocks or
+  // the lanes that select.
+  const int64_t lanes = (int64_t)v.H * dv::evict_select_lanes((int)longest);
+  const int64_t seqs = std::min({(int64_t)kQSeqs, kMaxItems / (v.H * blocks), UINT32_MAX / lanes});
 
   dv::EvictArgs a;
   memset(&a, 0, sizeof a);

@@ -32,20 +32,6 @@ struct QLayout {
   FastDiv d_bs;
 };
 
-// The smallest power of two, at least 2^-64, whose 448-fold is at least amax
-// (448 = 1.75 * 2^8): from amax's exponent, one more where its fraction exceeds
-// 1.75.
-__device__ __forceinline__ float scale_for(float amax) {
-  const uint32_t b = __float_as_uint(amax);
-  const int e = (int)(b >> 23) + ((b & 0x7fffff) > 0x600000) - 8;
-  return __uint_as_float((uint32_t)max(e, 127 - 64) << 23);
-}
-
-// 1 / p for a power of two of [2^-64, 2^120].
-__device__ __forceinline__ float inverse(float p) {
-  return __uint_as_float((254u << 23) - __float_as_uint(p));
-}
-
 // ---- dv_quant_in ----
 // A work item is one block of one head of one sequence; item[] counts those of
 // earlier sequences.  A group of 1 << lanes_log2 lanes takes an item, and each of
@@ -143,6 +129,8 @@ struct EvictArgs {
   int32_t item[kQSeqs];  // INT32_MAX past the last
 };
 static_assert(sizeof(EvictArgs) <= 3584, "arguments stay under 4 KB");
+// Lanes of a workgroup that selects (a head of a sequence): see the kernel.
+inline int evict_select_lanes(int most) { return most > 16 * 256 ? 1024 : 256; }
 hipError_t launch_evict_select(const EvictArgs& a, hipStream_t s);
 hipError_t launch_evict_move(const EvictArgs& a, hipStream_t s);
 

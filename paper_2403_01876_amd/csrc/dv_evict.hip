@@ -1,5 +1,6 @@
 // Eviction: which tokens of each head stay, and the compaction of what they own.
 #include "dv_attn_internal.h"
+#include "dv_scale.h"
 
 namespace dv {
 namespace {
@@ -359,13 +360,12 @@ __global__ void __launch_bounds__(kThreads) evict_move_large_kernel(EvictArgs a,
 
 hipError_t launch_evict_select(const EvictArgs& a, hipStream_t s) {
   // As few weights to a lane as hold the longest sequence.
-  const bool wide = a.most > 16 * 256;
-  const void* fn = wide                ? (const void*)&evict_select_kernel<1024, 16>
+  const int lanes = evict_select_lanes(a.most);
+  const void* fn = lanes == 1024      ? (const void*)&evict_select_kernel<1024, 16>
                    : a.most > 4 * 256 ? (const void*)&evict_select_kernel<256, 16>
                                       : (const void*)&evict_select_kernel<256, 4>;
   void* args[] = {const_cast<EvictArgs*>(&a)};
-  return hipLaunchKernel(fn, dim3((uint32_t)a.nseq * a.s.heads, a.nl), dim3(wide ? 1024 : 256),
-                         args, 0, s);
+  return hipLaunchKernel(fn, dim3((uint32_t)a.nseq * a.s.heads, a.nl), dim3(lanes), args, 0, s);
 }
 
 bool evict_blocks_held(int64_t bs, int64_t D) { return bs * D <= kHeld * 1024; }

@@ -10,6 +10,7 @@
 // tokens of 20 layers 6 us, of which 2 are the launch and the rest the way to a
 // block's place and scale.
 #include "dv_attn_internal.h"
+#include "dv_scale.h"
 
 namespace dv {
 namespace {
