@@ -6,7 +6,9 @@ sequence (dv_stream_out_token, dv_quant_in), runs every layer's attention, which
 accumulates the weight that each cached token receives (dv_attend), and, where a
 sequence has outgrown the budget, evicts the lightest tokens in place (dv_evict).
 Keys, values and queries are random, as a model's would be for the cache's
-purposes.  At the end the codes are streamed out as any cache's are.
+purposes.  At the end the cache is streamed into another pool, its codes as any
+cache's are and its scales as a cache of one head, whose "token" is a page's
+scales of all heads (so many heads as make 16 bytes or a multiple: 4, 8, ...).
 
     python examples/evicting_decode.py
 """
@@ -19,6 +21,17 @@ import torch
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
 from paper_2403_01876_amd import attn, dv  # noqa: E402
+
+
+def pool(layers, heads, dim, block, tables, codes, scales, **companions):
+    """An 8-bit paged cache, and its scales as a cache that streams too."""
+    batch, width = tables.shape
+    shape = dict(num_blocks=codes.shape[2], max_blocks=width, block_tables=[tables])
+    cache = attn.QuantCache(
+        dv.Cache(dv.DV_PAGED, layers, heads, dim, batch, [codes], elem_bytes=1, block_size=block,
+                 **shape), [scales], **{k: [v] for k, v in companions.items()})
+    return cache, dv.Cache(dv.DV_PAGED, layers, 1, heads, batch, [scales], elem_bytes=4,
+                           block_size=1, **shape)
 
 
 def main(layers=2, heads=4, group=2, dim=64, prompts=(90, 61, 128), steps=24, budget=96, keep=72,
@@ -41,10 +54,8 @@ def main(layers=2, heads=4, group=2, dim=64, prompts=(90, 61, 128), steps=24, bu
     scales = torch.ones((L, 2, pages, H), device="cuda")
     weights = torch.zeros((L, B, H, width * block), device="cuda")
     positions = torch.zeros((L, B, H, width * block), dtype=torch.int32, device="cuda")
-    cache = attn.QuantCache(
-        dv.Cache(dv.DV_PAGED, L, H, D, B, [codes], elem_bytes=1, block_size=block,
-                 num_blocks=pages, max_blocks=width, block_tables=[table]),
-        [scales], weights=[weights], positions=[positions])
+    cache, cache_scales = pool(L, H, D, block, table, codes, scales, weights=weights,
+                               positions=positions)
 
     length = np.array(prompts, np.int32)  # tokens in the 8-bit cache
     seen = length.copy()                  # tokens generated so far
@@ -57,7 +68,7 @@ def main(layers=2, heads=4, group=2, dim=64, prompts=(90, 61, 128), steps=24, bu
     kept = torch.full((L, B, H, max(max(prompts), budget) + 1), -1, dtype=torch.int32, device="cuda")
     one = np.ones(B, np.int32)
     q = torch.empty((B, H * group, D), dtype=torch.float16, device="cuda")
-    out = torch.empty((L, B, H * group, D), dtype=torch.float16, device="cuda")
+    out = torch.empty((max(L, 2), B, H * group, D), dtype=torch.float16, device="cuda")
     workspace = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
     evictions = 0
     for _ in range(steps):
@@ -83,17 +94,36 @@ def main(layers=2, heads=4, group=2, dim=64, prompts=(90, 61, 128), steps=24, bu
             x = x + slopes.view(H, group, 1) * (torch.arange(s, device="cuda") - (s - 1))
             ref = torch.einsum("hgt,htd->hgd", x.softmax(-1), v).reshape(H * group, D)
             worst = max(worst, float((out[l, b].float() - ref).norm() / ref.norm()))
-    replica = torch.empty(dv.dv_packed_bytes(cache.cache, 0, L, None, length), dtype=torch.uint8,
-                          device="cuda")
-    dv.dv_stream_out_prompt(cache.cache, 0, 0, L, None, length, replica, replica.numel())
+
+    # A replica: codes and scales go over a wire each into another pool, positions as
+    # they are (weights would too, if the replica is to evict by them).
+    blocks = -(-length // block)
+    other = torch.randperm(pages, device="cuda", generator=gen).to(torch.int32).view(B, width)
+    replica, replica_scales = pool(L, H, D, block, other, torch.empty_like(codes),
+                                   torch.empty_like(scales), positions=positions.clone())
+    sent = 0
+    for here, there, upto in ((cache.cache, replica.cache, length),
+                              (cache_scales, replica_scales, blocks)):
+        wire = torch.empty(dv.dv_packed_bytes(here, 0, L, None, upto), dtype=torch.uint8,
+                           device="cuda")
+        sent += dv.dv_stream_out_prompt(here, 0, 0, L, None, upto, wire, wire.numel())
+        dv.dv_stream_in(there, 0, 0, L, None, upto, wire, wire.numel())
+    same = True
+    for l in range(L):
+        for c, to in ((cache, out[0]), (replica, out[1])):
+            attn.dv_attend(c, 0, l, one, length, q, to, D ** -0.5, slopes=slopes,
+                           workspace=workspace)
+        same &= torch.equal(out[0], out[1])
     torch.cuda.synchronize()
     return {"length": length, "seen": seen, "evictions": evictions, "worst": worst,
-            "positions": positions, "replica_bytes": replica.numel(),
+            "positions": positions, "replica_bytes": sent, "replica_answers_the_same": same,
             "full_bytes": dv.dv_packed_bytes(source, 0, L, None, seen)}
 
 
 if __name__ == "__main__":
     r = main()
     print(f"{r['evictions']} evictions; tokens held {r['length'].tolist()} of {r['seen'].tolist()}")
-    print(f"replica {r['replica_bytes']} bytes, the 16-bit cache's {r['full_bytes']}")
+    print(f"replica {r['replica_bytes']} bytes, scales among them (the 16-bit cache's "
+          f"{r['full_bytes']}); it answers "
+          f"{'the same' if r['replica_answers_the_same'] else 'otherwise'}")
     print(f"attention differs from the whole 16-bit cache's by at most {r['worst']:.3f} (relative)")

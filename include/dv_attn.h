@@ -24,7 +24,7 @@ extern "C" {
 #endif
 
 /* An 8-bit cache.  Its codes lie in a dv_cache with elem_bytes 1, DV_DENSE or
- * DV_PAGED, in device memory, so everything of dv.h streams and swaps them.
+ * DV_PAGED, in device memory, so everything of dv.h streams and swaps the codes.
  * A code is an e4m3 number (sign, 4 exponent bits with bias 7, 3 fraction bits;
  * magnitudes 0 to 448, 0x7f and 0xff are NaN) and stands for code * scale; the
  * `scale_block` tokens of a block share one scale in each head, a power of two,
@@ -39,7 +39,15 @@ extern "C" {
  *             are not their slots (after an eviction).
  * capacity is max_seq, or max_blocks * block_size.  Each is a host array
  * [num_mb] of device addresses, or NULL; entries of the companions may be NULL
- * too.  Scales, weights and positions are 4-byte aligned. */
+ * too.  Scales, weights and positions are 4-byte aligned.
+ * A replica needs the scales as well as the codes.  Where they divide by 4 they
+ * are a dv_cache of their own with elem_bytes 4, which streams and swaps them
+ * (16-byte aligned then):
+ *   DV_PAGED  num_heads a multiple of 4: one head, head_dim num_heads, block_size
+ *             1, the same table; block j of a sequence is its token j
+ *   DV_DENSE  ceil(max_seq / scale_block) a multiple of 4: head_dim 4, max_seq a
+ *             quarter of it; blocks 4 j to 4 j + 3 are token j
+ * Weights and positions, without K|V halves, are not: copy them as arrays. */
 typedef struct dv_quant {
   const dv_cache* cache;
   int32_t scale_block;

@@ -173,3 +173,38 @@ def test_evict_between_pools_of_one_table():
     assert np.array_equal(kept.cpu().numpy(), want)
     assert np.array_equal(td["scale"].cpu().numpy(), d.scale)
     assert ref.same_codes(td["codes"].cpu().numpy(), d.codes)
+
+
+@pytest.mark.parametrize("kind", ["dense", "paged"])
+def test_scales_stream_as_a_cache(kind):
+    """As the header describes them: what arrives is the sender's, block by block."""
+    L, H, D, B, bs = 2, 4, 32, 3, 16
+    c = make(kind, L, H, D, B, 176, bs, 16)
+    d = make(kind, L, H, D, B, 176, bs, 17)
+    d.scale[...] = 3.0
+    lens, caches = np.array([170, 16, 0]), []
+    if kind == "dense":  # 11 blocks, so that 12 are allocated
+        for x in (c, d):
+            x.scale = np.concatenate([x.scale, x.scale[..., :1]], -1)
+    for x in (c, d):
+        t = {k: torch.from_numpy(v).cuda() for k, v in (("s", x.scale), ("t", x.table))
+             if v is not None}
+        caches.append((t, dv.Cache(dv.DV_PAGED, L, 1, H, B, [t["s"]], elem_bytes=4, block_size=1,
+                                   num_blocks=x.nblocks, max_blocks=x.mb, block_tables=[t["t"]])
+                       if kind == "paged" else
+                       dv.Cache(dv.DV_DENSE, L, H, 4, B, [t["s"]], elem_bytes=4, max_seq=3)))
+    (_, src), (td, dst) = caches
+    blocks = -(-lens // bs)
+    n = blocks if kind == "paged" else -(-blocks // 4)
+    wire = torch.empty(dv.dv_packed_bytes(src, 0, L, None, n), dtype=torch.uint8, device="cuda")
+    sent = dv.dv_stream_out_prompt(src, 0, 0, L, None, n, wire, wire.numel())
+    dv.dv_stream_in(dst, 0, 0, L, None, n, wire, sent)
+    got = td["s"].cpu().numpy()
+    for b in range(B):
+        for j in range(int(blocks[b])):
+            here, there = c.place(b, j), d.place(b, j)
+            if kind == "paged":
+                assert np.array_equal(got[:, :, there], c.scale[:, :, here])
+            else:
+                assert np.array_equal(got[:, :, b, :, there], c.scale[:, :, b, :, here])
+    assert (got == 3.0).any()

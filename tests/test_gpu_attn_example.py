@@ -37,3 +37,13 @@ def test_within_the_budget_nothing_is_lost_but_bits():
     r = load().main(budget=200)
     assert r["evictions"] == 0 and (r["length"] == r["seen"]).all()
     assert r["worst"] < 0.15
+
+
+@pytest.mark.parametrize("heads,layers", [(4, 2), (8, 1)])
+def test_the_replica_is_whole(heads, layers):
+    """Codes and scales as streamed into other pages give the same attention, bit for bit."""
+    r = load().main(heads=heads, layers=layers)
+    assert r["replica_answers_the_same"]
+    n = r["length"].astype(np.int64)
+    codes = int(n.sum()) * layers * 2 * heads * 64
+    assert r["replica_bytes"] == codes + int((-(-n // 16)).sum()) * layers * 2 * heads * 4
