@@ -69,13 +69,16 @@ def main(layers=2, heads=4, group=2, dim=64, prompts=(90, 61, 128), steps=24, bu
     one = np.ones(B, np.int32)
     q = torch.empty((B, H * group, D), dtype=torch.float16, device="cuda")
     out = torch.empty((max(L, 2), B, H * group, D), dtype=torch.float16, device="cuda")
-    workspace = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    workspace = torch.empty(0, dtype=torch.uint8, device="cuda")
     evictions = 0
     for _ in range(steps):
         m = dv.dv_stream_out_token(source, 0, 0, L, seen, wire, wire.numel())
         attn.dv_quant_in(cache, 0, 0, L, length, length + 1, wire, m, attn.DV_F16)
         length, seen = length + one, seen + one
         q.normal_(generator=gen)
+        need = attn.dv_attend_bytes(cache, one, length, q, weights=True)
+        if need > workspace.numel():  # as long as lengths grow, a little more each time
+            workspace = torch.empty(need * 5 // 4, dtype=torch.uint8, device="cuda")
         for l in range(L):
             attn.dv_attend(cache, 0, l, one, length, q, out[l], D ** -0.5, slopes=slopes,
                            decay=0.95, workspace=workspace)
@@ -109,6 +112,9 @@ def main(layers=2, heads=4, group=2, dim=64, prompts=(90, 61, 128), steps=24, bu
         sent += dv.dv_stream_out_prompt(here, 0, 0, L, None, upto, wire, wire.numel())
         dv.dv_stream_in(there, 0, 0, L, None, upto, wire, wire.numel())
     same = True
+    need = attn.dv_attend_bytes(cache, one, length, q)
+    if need > workspace.numel():
+        workspace = torch.empty(need, dtype=torch.uint8, device="cuda")
     for l in range(L):
         for c, to in ((cache, out[0]), (replica, out[1])):
             attn.dv_attend(c, 0, l, one, length, q, to, D ** -0.5, slopes=slopes,

@@ -47,3 +47,8 @@ def test_the_replica_is_whole(heads, layers):
     n = r["length"].astype(np.int64)
     codes = int(n.sum()) * layers * 2 * heads * 64
     assert r["replica_bytes"] == codes + int((-(-n // 16)).sum()) * layers * 2 * heads * 4
+
+
+def test_prompts_of_any_length():
+    r = load().main(layers=1, heads=8, group=4, prompts=(2500,) * 6, steps=2, budget=2501, keep=900)
+    assert r["evictions"] == 1 and (r["length"] == 900).all() and r["replica_answers_the_same"]
