@@ -208,3 +208,36 @@ def test_scales_stream_as_a_cache(kind):
             else:
                 assert np.array_equal(got[:, :, b, :, there], c.scale[:, :, b, :, here])
     assert (got == 3.0).any()
+
+
+@pytest.mark.parametrize("H,D,group", [(3, 128, 4), (2, 192, 20), (2, 96, 64)])
+def test_attend_codes_read_past_the_caches(H, D, group):
+    """Codes of 96 MB or more take loads of their own."""
+    n, bs = -(-(96 << 20) // (2 * H * D)), 16
+    pages = -(-n // bs)
+    gen = torch.Generator(device="cuda").manual_seed(D)
+    codes = torch.randint(0, 127, (1, 2, pages, H, bs, D), device="cuda", generator=gen)
+    codes += 128 * torch.randint(0, 2, codes.shape, device="cuda", generator=gen)
+    codes = codes.to(torch.uint8)
+    scale = torch.ldexp(torch.ones((), device="cuda"),
+                        torch.randint(-10, -7, (1, 2, pages, H), device="cuda", generator=gen))
+    table = torch.randperm(pages, device="cuda", generator=gen).to(torch.int32)[None].contiguous()
+    c = attn.QuantCache(
+        dv.Cache(dv.DV_PAGED, 1, H, D, 1, [codes], elem_bytes=1, block_size=bs, num_blocks=pages,
+                 max_blocks=pages, block_tables=[table]), [scale])
+    q = torch.randn((1, H * group, D), device="cuda", generator=gen).half()
+    out, lse = torch.empty_like(q), torch.empty((1, H * group), device="cuda")
+    ws = torch.empty(attn.dv_attend_bytes(c, [1], [n], q), dtype=torch.uint8, device="cuda")
+    attn.dv_attend(c, 0, 0, [1], [n], q, out, D ** -0.5, lse=lse, workspace=ws)
+    value = torch.from_numpy(ref.VALUE).cuda()
+    for h in range(H):
+        K, V = (value[codes[0, half, table[0].long(), h].long()].mul(
+            scale[0, half, table[0].long(), h].double()[:, None, None]).view(-1, D)[:n]
+            for half in (0, 1))
+        for g in range(h * group, (h + 1) * group):
+            s = K @ q[0, g].double() * D ** -0.5
+            p = torch.softmax(s, 0)
+            want, mass = p @ V, p @ V.abs()
+            tol = HALF["f16"] * want.abs() + PROB * mass + 2.0 ** -24
+            assert bool(((out[0, g].double() - want).abs() <= tol).all()), (h, g)
+            assert abs(float(lse[0, g]) - float(torch.logsumexp(s, 0))) <= 1e-5 * 20
