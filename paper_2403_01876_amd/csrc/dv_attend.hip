@@ -13,9 +13,10 @@
 // per query and sums relative to it.  m is set kLift below the largest score and
 // moves only when a score exceeds that by more than 8, so the common step needs no
 // exchange between lanes and no rescaling; probabilities then reach 2^(8 + kLift)
-// at most, which costs no precision.  kLift is 7 for f16, whose probabilities stay
+// at most, which costs no precision.  kLift is 7 for probabilities in f16, which stay
 // normal numbers down to 2^-21 of the largest so (a value 2^12 times another's
-// shows their rounding below 2^-14 otherwise), and 0 for bf16.
+// shows their rounding below 2^-14 otherwise), and -32 for those in bf16, which has
+// f32's range: their sums with values up to f32's largest stay below it.
 #include <algorithm>
 #include <type_traits>
 
@@ -79,7 +80,7 @@ struct Ty<false> {
 };
 template <>
 struct Ty<true> {
-  static constexpr float kLift = 0.f;
+  static constexpr float kLift = -32.f;
   template <bool HI>
   static __device__ __forceinline__ uint32_t cvt(uint32_t w, float s) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, HI));
@@ -130,6 +131,12 @@ __device__ __forceinline__ Seq seq_of(const AttendArgs& a, int item) {
   q.tok = __builtin_amdgcn_readlane(t0, q.b);
   q.nq = __builtin_amdgcn_readlane(t1, q.b) - q.tok;
   return q;
+}
+
+// log2 of the sum of a row's exponentials, from its sum relative to m.  (The lift is
+// taken off first: a logarithm of its size would have as many bits fewer.)
+__device__ __forceinline__ float lse2_of(float m, float sum, float lift) {
+  return (m + lift) + __log2f(sum * exp2_(-lift));
 }
 
 // Positions as numbers in 32 bits: less the last token's, so that distances are exact
@@ -506,8 +513,8 @@ __global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
       float most = s[rt][0][0];
 #pragma unroll
       for (int i = 1; i < 8; ++i) most = fmaxf(most, s[rt][i >> 2][i & 3]);
-      if (__any(most > m[rt] + kSlack)) {
-        float up = fmaxf(most, m[rt]);
+      if (__any(most > m[rt] + (kSlack + B::kLift))) {
+        float up = fmaxf(most - B::kLift, m[rt]);
         up = fmaxf(up, __shfl_xor(up, 16));
         up = fmaxf(up, __shfl_xor(up, 32));
         const float f = exp2_(m[rt] - up);
@@ -644,7 +651,7 @@ __global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
               u32x2{T::pack(v[0] * inv, v[1] * inv), T::pack(v[2] * inv, v[3] * inv)};
         if (a.lse && d == 0)
           a.lse[(int64_t)(a.row0 + seq.tok + i) * a.q_heads + head] =
-              total == 0.f ? -INFINITY : (top + __log2f(total)) * kLn2;
+              total == 0.f ? -INFINITY : lse2_of(top, total, B::kLift) * kLn2;
       }
     }
   }
@@ -659,7 +666,7 @@ __global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
       for (int w = 0; w < 4; ++w) top = fmaxf(top, mls[(w * RT * 16 + tid) * 2]);
       for (int w = 0; w < 4; ++w)
         total += mls[(w * RT * 16 + tid) * 2 + 1] * exp2_(mls[(w * RT * 16 + tid) * 2] - top);
-      lse2s[tid] = total == 0.f ? INFINITY : top + __log2f(total);
+      lse2s[tid] = total == 0.f ? INFINITY : lse2_of(top, total, B::kLift);
     }
     __syncthreads();
     add_weights(a, seq, sb, h, rows, c0, cn, lse2s, (f32x4*)(sums + 64));
@@ -1079,7 +1086,7 @@ __global__ void __launch_bounds__(kThreads, tile_waves(DP))
                                      T::pack(o[d][i + 2] * inv, o[d][i + 3] * inv)};
       }
     if (hf == 0) {
-      const float lse2 = m + __log2f(sum);
+      const float lse2 = lse2_of(m, sum, T::kLift);
       const int64_t row = (int64_t)(seq.tok + i0) * a.q_heads + head;
       if (a.lse) a.lse[(int64_t)a.row0 * a.q_heads + row] = sum == 0.f ? -INFINITY : lse2 * kLn2;
       if (a.weigh) a.row_lse[row] = sum == 0.f ? INFINITY : lse2;
@@ -1127,6 +1134,7 @@ __global__ void __launch_bounds__(kThreads) attend_join_kernel(AttendArgs a, int
   const int tile = tiles - 1 - scalar(kk / nsplit), split = kk - (tiles - 1 - tile) * nsplit;
   const int r0 = tile * R, nr = min(R, rows - r0);
   const float2* ml = (const float2*)a.ml + ((int64_t)item - split) * R;
+  const float lift = R == kTileRows ? T::kLift : Ty<true>::kLift;  // of the kernel before
 
   const int shares = gridDim.y - (a.scores ? 1 : 0), share = blockIdx.y;
   if (share < shares) {
@@ -1175,7 +1183,7 @@ __global__ void __launch_bounds__(kThreads) attend_join_kernel(AttendArgs a, int
                   (int64_t)head * a.o_head + d) =
             u32x2{T::pack(v[0] * inv, v[1] * inv), T::pack(v[2] * inv, v[3] * inv)};
       if (d == 0) {
-        const float lse2 = top + __log2f(total);
+        const float lse2 = lse2_of(top, total, lift);
         const int64_t row = (int64_t)(seq.tok + i) * a.q_heads + head;
         if (a.lse)
           a.lse[(int64_t)a.row0 * a.q_heads + row] = total == 0.f ? -INFINITY : lse2 * kLn2;
@@ -1199,7 +1207,7 @@ __global__ void __launch_bounds__(kThreads) attend_join_kernel(AttendArgs a, int
     sum *= exp2_(m - up);
 #pragma unroll
     for (int x = 16; x; x >>= 1) sum += __shfl_xor(sum, x);
-    if (tid % 32 == 0) lse2s[r] = sum == 0.f ? INFINITY : up + __log2f(sum);
+    if (tid % 32 == 0) lse2s[r] = sum == 0.f ? INFINITY : lse2_of(up, sum, lift);
   }
   __syncthreads();
   add_weights(a, seq, sb, h, nr, split * a.chunk, min(a.chunk, len - split * a.chunk), lse2s,

@@ -120,6 +120,41 @@ def test_attend_few_rows_keep_numbers_beyond_f16():
     run_attend(c, [1, 1], [300, 211], 2, "f16", decay=0.0, spread=2.0 ** -16)
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("tokens,length", [(1, 200), (70, 200), (1, 3000), (70, 3000)])
+def test_attend_one_value_as_large_as_can_be(dtype, tokens, length):
+    """What an infinity of a bf16 stream becomes, seen by rows that give it about half
+    (or less) of their weight after smaller scores: finite, and in its own dimension."""
+    c = make("dense", 1, 1, 64, 1, length, 16, 18)
+    c.codes[0, 0] = 0
+    c.codes[0, 0, 0, 0, 150] = ref.encode(np.array(0.6875))
+    c.scale[0, 0] = 1.0
+    big = c.codes[0, 1, 0, 0, 144:160]  # the block around slot 150
+    big[...] = 0
+    big[6, 5] = ref.encode(np.array(240.0))
+    c.scale[0, 1, 0, 0, 9] = 2.0 ** 120
+    d, _ = c.device(dv, attn)
+    q = torch.ones((tokens, 1, 64), dtype=ref.TDTYPE[dtype], device="cuda")
+    out = torch.empty_like(q)
+    nb = attn.dv_attend_bytes(d, [tokens], [length], q)
+    ws = torch.empty(nb, dtype=torch.uint8, device="cuda")
+    attn.dv_attend(d, 0, 0, [tokens], [length], q, out, 0.125, workspace=ws)
+    if dtype == "f16" and tokens > 64:  # its largest number, there
+        c = Saturated.__new__(Saturated)
+        c.__dict__.update(make("dense", 1, 1, 64, 1, length, 16, 18).__dict__)
+        c.codes[0, 0], c.scale[0, 0] = 0, 1.0
+        c.codes[0, 0, 0, 0, 150] = ref.encode(np.array(0.6875))
+        c.codes[0, 1, 0, 0, 144:160] = big
+        c.scale[0, 1, 0, 0, 9] = 2.0 ** 120
+    want, mass, _, _ = ref.attend(c, 0, [tokens], [length], q.double().cpu().numpy(), 0.125)
+    y = out.double().cpu().numpy()
+    past = np.abs(want) > 65520.0 if dtype == "f16" else np.zeros(want.shape, bool)
+    assert np.isinf(y[past]).all()
+    tol = HALF[dtype] * np.abs(want) + (PROB + (HALF[dtype] if tokens > 64 else 0)) * mass + 2.0 ** -24
+    assert np.all(np.abs(y - want)[~past] <= tol[~past])
+    assert np.abs(want).max() > 1000
+
+
 # ---- positions past 2^24, scores past 1e30 ---------------------------------------------------
 
 
