@@ -156,7 +156,11 @@ def dv_attend(c: QuantCache, mb: int, layer: int, q_len, kv_len, q, out, scale: 
     if lse is not None:
         _floats("lse", lse, (min(rows, lse.shape[0]), heads))
         rows, lse = min(rows, lse.shape[0]), lse.data_ptr()
-    wb = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    wb = 0
+    if workspace is not None:
+        if not workspace.is_contiguous():
+            raise ValueError(f"workspace must be contiguous, got strides {workspace.stride()}")
+        wb = workspace.numel() * workspace.element_size()
     a = dv_attend_args(_TYPES[q.dtype], heads, scale, 0.0 if decay is None else decay,
                        decay is not None, rows, q.data_ptr(), out.data_ptr(), qt, qh, ot, oh,
                        slopes, lse, _addr(workspace), wb)

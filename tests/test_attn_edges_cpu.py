@@ -5,6 +5,7 @@ import re
 
 import numpy as np
 import pytest
+import torch
 
 from paper_2403_01876_amd import attn, dv
 from tests.test_attn_cpu import (FAKE, INVALID, KEPT, POS, SCALE, SPACE, TABLE, UNSUPPORTED, WEIGHT,
@@ -63,3 +64,13 @@ def test_inline_assembly_names_the_registers_it_writes():
     assert len(writes) == 3
     for b in writes:
         assert re.search(r':[^:]*"m0"[^:]*$', b), b
+
+
+def test_a_workspace_with_gaps_is_refused():
+    """Its bytes are counted as one range."""
+    c = dv.Cache(dv.DV_DENSE, 1, 2, 64, 1, [FAKE], elem_bytes=1, max_seq=40)
+    qc = attn.QuantCache(c, [SCALE], scale_block=16)
+    q = torch.zeros((1, 4, 64), dtype=torch.float16)
+    for ws in (torch.zeros(64, dtype=torch.uint8)[::2], torch.zeros(1).expand(64)):
+        with pytest.raises(ValueError, match="workspace must be contiguous"):
+            attn.dv_attend(qc, 0, 0, [1], [4], q, q.clone(), 1.0, workspace=ws)
