@@ -32,7 +32,8 @@ extern "C" {
  *   DV_DENSE  scale[layer][K|V][batch][head][ceil(max_seq / scale_block)],
  *             token s in block s / scale_block
  *   DV_PAGED  scale[layer][K|V][num_blocks][head]; scale_block == block_size
- * A scale that is not a positive power of two gives unspecified results.
+ * A scale that is not a power of two of [2^-64, 2^120] gives unspecified results
+ * where a token of its block is used; blocks that no table names may hold anything.
  * Two optional companions go by slots (a token's place in its sequence):
  *   weight    [layer][batch][head][capacity]: accumulated attention weight;
  *   position  [layer][batch][head][capacity]: the tokens' positions, where they
@@ -125,10 +126,14 @@ DV_API int dv_attend_bytes(const dv_quant* c, const int32_t* q_len, const int32_
  * (with decay 0 the old weight is not read); sequences without queries keep
  * their weights.  Codes past a query's slot do not enter its result, NaN or
  * not; slots in unmapped blocks are not seen.  Scores, sums and weights are kept
- * in 32 bits.  Where a sequence of the call has more than 64 rows (q_len times G;
- * 32 for head_dim above 128), cached numbers are read in the queries' type: f16
- * takes those beyond it (of a cache rounded from bf16) as its largest and those
- * of the smallest magnitudes to a multiple of 2^-24.
+ * in 32 bits (a weight errs by as much as a score and its row's log-sum do, 2^-23 of
+ * them).
+ * The most rows of a sequence (q_len times G) decide for the call how
+ * probabilities and cached numbers enter the products.  Up to 64 (32 for head_dim
+ * above 128) probabilities keep 16 bits, and cached numbers all of theirs whatever
+ * the queries' type.  Beyond, both are rounded to the queries' type: half a step of
+ * it for a probability; f16 takes numbers beyond it (of a cache rounded from bf16)
+ * as its largest and the smallest as multiples of 2^-24.
  * head_dim at most 256 (DV_ERR_UNSUPPORTED); one layer's keys at most 64 GB.
  * Results do not depend on the order in which workgroups run.  q, the cache and
  * its table are not written; out, lse, workspace and weights must not overlap

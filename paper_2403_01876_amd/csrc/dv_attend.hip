@@ -272,11 +272,12 @@ __device__ __forceinline__ void add_weights(const AttendArgs& a, const Seq& seq,
 // product runs in bf16 for either type (codes are exact in it, and so is the
 // range of scaled probabilities), with each probability as the sum of two
 // numbers, which keeps 16 bits of it; the matrix unit has time to spare.
-// Bound by HBM and, per workgroup, by about 6 us before the first product (launch,
-// table entries, scales, the first codes) and after the last (the waves' results):
-// 32 sequences of 128 to 4096 tokens, 8 heads, 140 MB 30 us, 4.6 TB/s; one of
-// 131071, 273 MB (and 34 MB of scores written) 64 us, 4.8 TB/s.  The same bytes
-// read in random pieces of 2 KB and not used take 25 and 47 us.
+// Bound by HBM and, per workgroup, by what comes before the first product (table
+// entries, scales, the first codes, one after another) and after the last (the
+// waves' results): 32 sequences of 128 to 4096 tokens, 8 heads, 140 MB 29 us, 4.8
+// TB/s; one of 131071, 273 MB (and 34 MB of scores written) 62 us, 4.9 TB/s.  A
+// wave lives for 54 % of the first and 72 % of the second; 59 % of the 56 us of 64
+// rows (143 MB), whose registers hold two workgroups a CU.
 // ---------------------------------------------------------------------------
 // 16 bytes a lane from memory to LDS: to lds + 16 * lane.
 template <bool NT>
@@ -690,11 +691,15 @@ __global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
 // the next tile's scores and the products with its values.
 // Places and scales of 256 tokens (a segment) stand in LDS; the next segment's are
 // brought in between: table entries, then scales, by the same kind of copy.
-// Bound by the matrix units, the exponentials and LDS, which take turns within a
-// wave more than they overlap: 4 sequences of 1500 to 4000 tokens, the last 700 to
-// 1024 queries of 8 heads of 8 each, 265 GFLOP 0.43 ms, 0.61 PFLOP/s, half of
-// what a large matrix product reaches.  64 rows a wave instead of 32 took 0.69 ms
-// (results moved between register files), 64 tokens a tile 0.54 (spilled).
+// Probabilities are rounded to the queries' type for the second product: in bf16, 4
+// sequences of 1500 to 4000 tokens, the last 700 to 1024 queries of 8 heads of 8
+// each, are 2.3e-3 from 64 bits (rounding the result alone, 1.7e-3) in 382 us a
+// call; with each as the sum of two numbers it took 472.
+// Bound by the matrix units, vector instructions and LDS, which are busy 27, 36 and
+// 38 % of that time and take turns within a wave more than they overlap: 265 GFLOP
+// 0.385 ms, 0.69 PFLOP/s, 57 % of what a large matrix product reaches.  (When this
+// took 0.51 ms, 64 rows a wave instead of 32 took 0.69, results moved between
+// register files, and 64 tokens a tile 0.54, spilled.)
 // ---------------------------------------------------------------------------
 constexpr int kTile = 32, kSegment = 256, kPerSegment = kSegment / kTile, kAhead = 4;
 
@@ -1222,7 +1227,8 @@ __global__ void __launch_bounds__(kThreads) attend_join_kernel(AttendArgs a, int
 // pieces stored at piece ^ key(row), as above).  Each sum is one lane's; the
 // lanes', then the two waves', are added in a fixed order.
 // Bound by the exponentials and the product: 132 GFLOP (the case of the tile kernel)
-// 0.25 ms, 0.53 PFLOP/s.  Three heads, 1647 tokens, up to 413 queries
+// 0.22 ms, 0.60 PFLOP/s, the matrix units busy 24 % of the time and vector
+// instructions 48 %.  Three heads, 1647 tokens, up to 413 queries
 // of 16: 52 us in shares of the rows and 5 to add them, 216 without shares.
 // ---------------------------------------------------------------------------
 template <bool BF16, int DP>

@@ -208,8 +208,12 @@ __device__ __forceinline__ u32x4 again(u32x4 c, float ratio) {
 // block's tokens come from its own slots or later ones, so once the four waves
 // have read, what they write over is no longer needed.
 // Bound by HBM: 286 MB (32 sequences of 128 to 4096 tokens, 8 heads of 128, half
-// stay) 76 us, 3.8 TB/s, of rows of 128 bytes from places that the weights choose.
+// stay) 75 us, 3.8 TB/s, of rows of 128 bytes from places that the weights choose;
+// 148 MB are read and 140 written, no more than the work needs.
 // Stores go past the caches: 75.6 us, through them 78.6.
+// On the same buffers each time, the eviction takes 74 us a call, and in place, with
+// positions and weights to move too, 151; of one sequence of 131071 tokens, 8 heads,
+// 0.36 ms and 3.4.
 // ---------------------------------------------------------------------------
 constexpr int kHeld = 4;  // units of 16 codes that a lane holds: a block has 64 times as many
 
@@ -310,6 +314,7 @@ __global__ void __launch_bounds__(kThreads) evict_move_kernel(EvictArgs a) {
 // The same for blocks too large to be held, read again after their scale is known.
 // In place a workgroup is one wave and takes a head's blocks in order, 64 units of
 // a block in order: what it writes over has been read.
+// Blocks of 64 tokens instead of 16 in the case above: 134 us a call, in place 349.
 __global__ void __launch_bounds__(kThreads) evict_move_large_kernel(EvictArgs a, int groups) {
   const int l = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   const int g = blockIdx.x % (uint32_t)groups, bh = blockIdx.x / (uint32_t)groups;

@@ -2,12 +2,13 @@
 // scale for each block of tokens of a head.
 //
 // A block's elements are contiguous in the stream and, one byte each, in the
-// cache.  A group of lanes holds them in registers while it finds the largest
-// magnitude, so that each is read once; blocks too large for that are read
-// again (from L2).
+// cache.  A group of lanes, a wave at most, holds them in registers while it finds the
+// largest magnitude, so that each is read once; blocks too large for that are read
+// again (from L2): the prompts below, on the same buffers each time, take 65 us a call
+// with a scale for 16 tokens, 73 for 64 and 184 for 1024.
 // Bound by HBM: 2 bytes read and 1 written per element.  378 MB (8 prompts of 512
 // to 1024 tokens, 40 heads of 128, two layers) 68 us, 5.6 TB/s; a step's 32
-// tokens of 20 layers 6 us, of which 2 are the launch and the rest the way to a
+// tokens of 20 layers 5 us, of which 2 are the launch and the rest the way to a
 // block's place and scale.
 #include "dv_attn_internal.h"
 #include "dv_scale.h"
