@@ -133,19 +133,10 @@ def dv_attend_bytes(c: QuantCache, q_len, kv_len, q, weights: bool = False,
     return out.value if check else (rc, out.value)
 
 
-def dv_attend(c: QuantCache, mb: int, layer: int, q_len, kv_len, q, out, scale: float,
-              slopes=None, decay: Optional[float] = None, lse=None, workspace=None, stream=None,
-              check: bool = True) -> int:
-    """Attention of the queries ``q`` [tokens, q_heads, head_dim] into ``out`` (any
-    strides that are multiples of 8, rows contiguous).  ``decay``: accumulate
-    the cache's weights, those from before times this (None: do not).  ``lse``: a
-    float32 [tokens, q_heads] tensor.  ``workspace``: a tensor of dv_attend_bytes
-    bytes."""
-    cache = c.cache.c
-    a0, p0 = _i32(q_len, cache.batch)
-    a1, p1 = _i32(kv_len, cache.batch)
-    rows, heads, qt, qh = _rows("q", q, cache.head_dim)
-    out_rows, out_heads, ot, oh = _rows("out", out, cache.head_dim)
+def _attend_args(c: QuantCache, q, out, scale, slopes, decay, lse, workspace):
+    dim = c.cache.c.head_dim
+    rows, heads, qt, qh = _rows("q", q, dim)
+    out_rows, out_heads, ot, oh = _rows("out", out, dim)
     if out_heads != heads or out.dtype is not q.dtype:
         raise ValueError(f"q {tuple(q.shape)} {q.dtype}, out {tuple(out.shape)} {out.dtype}")
     if out_rows < rows:
@@ -161,9 +152,23 @@ def dv_attend(c: QuantCache, mb: int, layer: int, q_len, kv_len, q, out, scale: 
         if not workspace.is_contiguous():
             raise ValueError(f"workspace must be contiguous, got strides {workspace.stride()}")
         wb = workspace.numel() * workspace.element_size()
-    a = dv_attend_args(_TYPES[q.dtype], heads, scale, 0.0 if decay is None else decay,
-                       decay is not None, rows, q.data_ptr(), out.data_ptr(), qt, qh, ot, oh,
-                       slopes, lse, _addr(workspace), wb)
+    return dv_attend_args(_TYPES[q.dtype], heads, scale, 0.0 if decay is None else decay,
+                          decay is not None, rows, q.data_ptr(), out.data_ptr(), qt, qh, ot, oh,
+                          slopes, lse, _addr(workspace), wb)
+
+
+def dv_attend(c: QuantCache, mb: int, layer: int, q_len, kv_len, q, out, scale: float,
+              slopes=None, decay: Optional[float] = None, lse=None, workspace=None, stream=None,
+              check: bool = True) -> int:
+    """Attention of the queries ``q`` [tokens, q_heads, head_dim] into ``out`` (any
+    strides that are multiples of 8, rows contiguous).  ``decay``: accumulate
+    the cache's weights, those from before times this (None: do not).  ``lse``: a
+    float32 [tokens, q_heads] tensor.  ``workspace``: a tensor of dv_attend_bytes
+    bytes."""
+    cache = c.cache.c
+    a0, p0 = _i32(q_len, cache.batch)
+    a1, p1 = _i32(kv_len, cache.batch)
+    a = _attend_args(c, q, out, scale, slopes, decay, lse, workspace)
     rc = _attend(c.ref, mb, layer, p0, p1, _byref(a), _stream(stream))
     return _check(rc, "dv_attend", check)
 

@@ -28,7 +28,8 @@ def _run(cmd):
 
 
 SOURCES = ("dv_attend.hip", "dv_kernels.hip", "dv_api.cpp", "dv_swapper.cpp", "dv_streamer.cpp",
-           "dv_noalloc.hip", "dv_attn.cpp", "dv_quant.hip", "dv_evict.hip")
+           "dv_noalloc.hip", "dv_attn.cpp", "dv_quant.hip", "dv_evict.hip", "dv_verify.hip",
+           "dv_draft.hip", "dv_draft.cpp")
 
 
 def build_libdv(out: str = LIBDV, flags=()) -> str:

@@ -184,6 +184,94 @@ __device__ __forceinline__ float sum_of_half(float x) {
   return x + __shfl_xor(x, 16);
 }
 
+// Drafted tokens as a tree (the last nq slots of a sequence): lane l has, of draft l
+// (and of draft l + 64 where there are more than 64), the set of itself and its
+// ancestors, or none where its line does not end at a draft that follows the slots
+// before (parent -1).  Parents come before their children, so one round through
+// memory and log2(nq) of exchanges between lanes, each of which doubles how far up a
+// line is known, find all.
+struct Line {
+  uint64_t lo, hi;  // drafts 0 to 63, 64 to 127
+  __device__ __forceinline__ bool there() const { return (lo | hi) != 0; }
+  __device__ __forceinline__ int depth() const { return __popcll(lo) + __popcll(hi) - 1; }
+  // Bit i: whether draft d0 + i is of the set, or for negative numbers, a slot
+  // before all drafts, whether it is seen (d0 the same in all lanes, or not).
+  __device__ __forceinline__ uint32_t from(int d0) const {
+    if (d0 >= 0) {
+      const uint64_t x = d0 < 64 ? lo >> d0 : d0 < 128 ? hi >> (d0 - 64) : 0;
+      return (uint32_t)x | (d0 > 32 && d0 < 64 ? (uint32_t)(hi << (64 - d0)) : 0u);
+    }
+    const uint32_t seen = there() ? ~0u : 0u;
+    return d0 <= -32 ? seen : (seen & ((1u << -d0) - 1)) | (uint32_t)(lo << -d0);
+  }
+};
+struct Tree {
+  Line a, b;
+  bool gone;  // whether some draft is not there
+};
+__device__ __forceinline__ uint64_t shfl64(uint64_t x, int from) {
+  return (uint64_t)(uint32_t)__shfl((int)(x >> 32), from) << 32 |
+         (uint32_t)__shfl((int)x, from);
+}
+template <bool WIDE>
+__device__ __forceinline__ Tree tree_of(const int32_t* parent, int nq) {
+  const int l = threadIdx.x & 63;
+  Tree t;
+  int p = l < nq ? parent[l] : -2;
+  if (p < -1 || p >= l) p = -2;
+  t.a = Line{1ull << l, 0};
+  t.b = Line{0, 1ull << l};
+  int p2 = -2;
+  if (WIDE && nq > 64) {
+    p2 = l + 64 < nq ? parent[l + 64] : -2;
+    if (p2 < -1 || p2 >= l + 64) p2 = -2;
+  }
+  for (int k = 1; k < nq; k <<= 1) {
+    const int at = max(p, 0) & 63;
+    const uint64_t up = shfl64(t.a.lo, at);
+    const int next = __shfl(p, at);
+    if (WIDE && nq > 64) {  // from what the first 64 were before this round
+      const int at2 = max(p2, 0) & 63;
+      const uint64_t x = shfl64(t.a.lo, at2), lo = shfl64(t.b.lo, at2), hi = shfl64(t.b.hi, at2);
+      const int y = __shfl(p, at2), z = __shfl(p2, at2);
+      if (p2 >= 0) {
+        t.b.lo |= p2 < 64 ? x : lo;
+        t.b.hi |= p2 < 64 ? 0 : hi;
+        p2 = p2 < 64 ? y : z;
+      }
+    }
+    if (p >= 0) {
+      t.a.lo |= up;
+      p = next;
+    }
+  }
+  if (p < -1) t.a.lo = 0;
+  if (p2 < -1) t.b.lo = t.b.hi = 0;
+  t.gone = __any((l < nq && p < -1) || (WIDE && l + 64 < nq && p2 < -1));
+  return t;
+}
+// The line of draft i (any, in every lane of the wave).
+template <bool WIDE>
+__device__ __forceinline__ Line line_of(const Tree& t, int i) {
+  Line x{shfl64(t.a.lo, i & 63), 0};
+  if constexpr (WIDE) {
+    const Line y{shfl64(t.b.lo, i & 63), shfl64(t.b.hi, i & 63)};
+    if (i >= 64) x = y;
+  }
+  return x;
+}
+// The same for one draft and one slot (d: slots from the first draft's), by a walk.
+__device__ __forceinline__ bool draft_sees(const int32_t* parent, int i, int d) {
+  bool seen = d < 0;
+  for (;;) {
+    seen |= i == d;
+    const int p = parent[i];
+    if (p == -1) return seen;
+    if (p < -1 || p >= i) return false;
+    i = p;
+  }
+}
+
 // 0x80 in each byte of w that is a NaN code.
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
   return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
@@ -205,6 +293,7 @@ __device__ __forceinline__ void spread_nan(const AttendArgs& a, int sb, int h, i
       const int j = q.d_bs.div(t);
       const int64_t blk = q.bt ? q.bt[(int64_t)sb * q.max_blocks + j] : j;
       if (q.bt && (uint64_t)blk >= (uint64_t)q.num_blocks) continue;
+      if (a.parent && !draft_sees(a.parent + tok, i, t - (len - nq))) continue;
       nan |= (vb[blk * q.s_blk + (int64_t)(t - j * q.bs) * q.D + d] & 127) == 127;
     }
     if (!nan) continue;
@@ -305,7 +394,7 @@ __device__ __forceinline__ u32x2 read_tr8(const uint8_t* p) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)p));
 }
 
-template <bool BF16, int DP, int RT>
+template <bool BF16, int DP, int RT, bool TREE>
 __global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
     attend_split_kernel(AttendArgs a, int direct) {
   using T = Ty<BF16>;
@@ -334,14 +423,20 @@ __global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
   float* ks = tables + a.chunk;       // key scales times the scores' factor; NaN: unmapped
   float* vs = tables + 2 * a.chunk;   // value scales
   float* pos = tables + 3 * a.chunk;
-  f32x4* columns = (f32x4*)(tables + (a.slopes ? 4 : 3) * a.chunk);  // limit, slope, position
+  // each column's limit, slope, position; of a tree, its line in place of the limit
+  f32x4* columns = (f32x4*)(tables + (a.slopes ? 4 : 3) * a.chunk);
   int* odd = (int*)(columns + RT * 16);
+  const int base = len - nq;  // the queries' first slot
+  Tree tree;
+  if constexpr (TREE) tree = tree_of<false>(a.parent + seq.tok, nq);
   const int64_t slab = 2 * (int64_t)a.layer;
   const uint8_t* kb = q.codes + slab * q.s_slab + sb * q.s_b + h * q.s_h;
   const uint8_t* vb = kb + q.s_slab;
   const float* sk = q.scale + slab * q.c_slab + sb * q.c_b + h * q.c_h;
   const int64_t slots = (((int64_t)a.layer * q.batch + sb) * q.heads + h) * (int64_t)q.cap;
-  const int last_at = last_position(q, a.slopes, slots, len);
+  const int last_at = last_position(q, a.slopes, slots, TREE ? base : len);
+  // a draft's position: this and its depth
+  const int root_at = q.position ? base > 0 : base;
   int bad = 0;
   for (int i = tid; i < ((cn + kSplitStep - 1) & -kSplitStep); i += kThreads) {
     const int t = min(c0 + i, len - 1), j = q.d_bs.div(t);
@@ -354,8 +449,14 @@ __global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
     }
     off[i] = (uint32_t)((blk * q.s_blk + (int64_t)(t - j * q.bs) * q.D) >> 4);
     ((int*)ks)[i] = hole ? -1 : (int)blk;
-    if (a.slopes) pos[i] = q.position ? from_last(q.position[slots + t], last_at) : (float)t;
+    if (a.slopes && !(TREE && t >= base))
+      pos[i] = q.position ? from_last(q.position[slots + t], last_at) : (float)t;
     bad |= hole;
+  }
+  if constexpr (TREE) {
+    const int i = base + l - c0;
+    if (a.slopes && wave == 0 && l < nq && i >= 0 && i < cn)
+      pos[i] = (float)(root_at + tree.a.depth());
   }
 
   // The queries, and what each column (row c of tile rt) may see.
@@ -375,14 +476,22 @@ __global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
       if constexpr (!kInLds) qr[rt][s] = x;
       if (kInLds && mine) ql[(rt * KS + s) * 64] = x;
     }
+    Line line{0, 0};
+    if constexpr (TREE) line = line_of<false>(tree, i);
     if (mine && g == 0) {
       const int limit = on ? len - nq + i : -1;
       float slope = 0.f, here = 0.f;
-      if (a.slopes && limit >= 0) {
+      if (a.slopes && limit >= 0 && !(TREE && !line.there())) {
         slope = a.slopes[head] * kLog2e;
-        here = q.position ? from_last(q.position[slots + limit], last_at) : (float)limit;
+        here = TREE         ? (float)(root_at + line.depth())
+               : q.position ? from_last(q.position[slots + limit], last_at)
+                            : (float)limit;
       }
-      columns[r] = f32x4{__int_as_float(limit), slope, here, 0.f};
+      if constexpr (TREE)
+        columns[r] = f32x4{__uint_as_float(on ? (uint32_t)line.lo : 0u), slope, here,
+                           __uint_as_float(on ? (uint32_t)(line.lo >> 32) : 0u)};
+      else
+        columns[r] = f32x4{__int_as_float(limit), slope, here, 0.f};
     }
   }
   // (LDS is all that the workgroup shares so far: loads may stay in flight)
@@ -390,7 +499,8 @@ __global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
   if (l == 0) odd[wave] = any_bad;
   lds_barrier();
   const bool holes = odd[0] | odd[1] | odd[2] | odd[3];
-  const int all_see = len - nq;  // slots up to this one are seen by every row
+  // slots up to this one are seen by every row
+  const int all_see = !TREE ? len - nq : tree.gone ? -1 : base - 1;
 
   // Copy n of a half: tokens n * 64 / CH ..., lane's token l / CH of them, piece
   // l % CH of its place.  Pieces past head_dim repeat the row's first one: they
@@ -502,12 +612,18 @@ __global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
         }
       }
       if (mask) {
-        const int limit = __float_as_int(columns[rt * 16 + c][0]);
+        const f32x4 column = columns[rt * 16 + c];
+        const int limit = __float_as_int(column[0]);
+        uint32_t mine = 0;
+        if constexpr (TREE)
+          mine = Line{(uint64_t)__float_as_uint(column[3]) << 32 | __float_as_uint(column[0]), 0}
+                     .from(c0 + t - base) >> (g * 4);
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const bool sees = first + u * 16 + r <= limit && kscale[u][r] == kscale[u][r];
+            const bool up_to = TREE ? (mine >> (u * 16 + r)) & 1 : first + u * 16 + r <= limit;
+            const bool sees = up_to && kscale[u][r] == kscale[u][r];
             s[rt][u][r] = sees ? s[rt][u][r] : -INFINITY;
           }
       }
@@ -728,9 +844,10 @@ struct TileLds {
   static constexpr int kTables = kCodes + kAhead * kRaw, kTable = 5 * kSegment * 4;
   static constexpr int kFlags = kTables + 2 * kTable;  // holes [2][4], NaN [4][2]
   static constexpr int kBytes = kFlags + 16 * 4;
+  static constexpr int kDrafts = kBytes, kTreeBytes = kBytes + kMaxDrafts * 4;  // their positions
 };
 
-template <bool BF16, int DP>
+template <bool BF16, int DP, bool TREE>
 __global__ void __launch_bounds__(kThreads, tile_waves(DP))
     attend_tile_kernel(AttendArgs a, int direct) {
   using T = Ty<BF16>;
@@ -757,8 +874,16 @@ __global__ void __launch_bounds__(kThreads, tile_waves(DP))
   const int r0 = tile * kTileRows, r = r0 + wave * 32 + c;
   const bool on = r < rows;
   const int i0 = r / a.G, head = h * a.G + (r - i0 * a.G);
-  const int limit = on ? len - nq + i0 : -1;
-  const int all_see = len - nq + scalar(r0 / a.G);
+  const int base = len - nq;  // the queries' first slot
+  Tree tree;
+  Line line{0, 0};
+  if constexpr (TREE) {
+    tree = tree_of<true>(a.parent + seq.tok, nq);
+    line = line_of<true>(tree, on ? i0 : 0);
+    if (!on) line = Line{0, 0};
+  }
+  const int limit = !on || (TREE && !line.there()) ? -1 : base + i0;
+  const int all_see = !TREE ? base + scalar(r0 / a.G) : tree.gone ? -1 : base - 1;
   const int last = len - nq + scalar((min(rows, r0 + kTileRows) - 1) / a.G);  // last slot seen
   const int begin = split * a.chunk, end = min(min(begin + a.chunk, len), last + 1);
   const int N = end > begin ? (end - begin + kTile - 1) / kTile : 0;
@@ -785,8 +910,20 @@ __global__ void __launch_bounds__(kThreads, tile_waves(DP))
   // (A factor of 0 makes equal scores; as a tiny one it leaves hidden ones at -infinity.)
   const float factor = fmaxf(fabsf(a.scale2), 0x1p-126f);
   float slope = 0.f, here = 0.f;
-  const int last_at = last_position(q, a.slopes, slots, len);
-  if (a.slopes && limit >= 0) {
+  const int last_at = last_position(q, a.slopes, slots, TREE ? base : len);
+  float* const draft_at = (float*)(lds + L::kDrafts);
+  if constexpr (TREE) {
+    const int root_at = q.position ? base > 0 : base;  // a draft's position: this and its depth
+    if (a.slopes && limit >= 0) {
+      slope = a.slopes[head] * kLog2e;
+      here = (float)(root_at + line.depth());
+    }
+    if (a.slopes && wave == 0) {  // (before the first barrier; read after it)
+      draft_at[l] = (float)(root_at + tree.a.depth());
+      draft_at[l + 64] = (float)(root_at + tree.b.depth());
+    }
+    __syncthreads();
+  } else if (a.slopes && limit >= 0) {
     slope = a.slopes[head] * kLog2e;
     here = q.position ? from_last(q.position[slots + limit], last_at) : (float)limit;
   }
@@ -808,7 +945,8 @@ __global__ void __launch_bounds__(kThreads, tile_waves(DP))
     ((int*)table(g, kEntry))[tid] = hole ? -1 : 0;
     const bool any = __any(hole);
     if (l == 0) holes_of[(g & 1) * 4 + wave] = any;
-    if (a.slopes && !q.position) table(g, kPosition)[tid] = (float)slot;
+    if (a.slopes && !q.position)
+      table(g, kPosition)[tid] = TREE && slot >= base ? draft_at[slot - base] : (float)slot;
     return blk;
   };
 
@@ -913,7 +1051,9 @@ __global__ void __launch_bounds__(kThreads, tile_waves(DP))
     table(0, kKeyScale)[tid] = sk[blk * q.c_blk];
     table(0, kValueScale)[tid] = sk[blk * q.c_blk + q.c_slab];
     if (a.slopes && q.position)
-      table(0, kPosition)[tid] = from_last(q.position[slots + slot], last_at);
+      table(0, kPosition)[tid] = TREE && slot >= base
+                                     ? draft_at[slot - base]
+                                     : from_last(q.position[slots + slot], last_at);
     __syncthreads();
     holes = any_hole(0);
     for (int n = 0; n < kAhead; ++n) fetch(n, N - 1);
@@ -941,7 +1081,8 @@ __global__ void __launch_bounds__(kThreads, tile_waves(DP))
         next_holes = any_hole(g + 1);
         if (a.slopes && q.position) {  // what this lane asked for
           float* x = table(g + 1, kPosition) + tid;
-          *x = from_last(*(const int*)x, last_at);
+          const int slot = slot_of(g + 1);
+          *x = TREE && slot >= base ? draft_at[slot - base] : from_last(*(const int*)x, last_at);
         }
       }
       if (n % kPerSegment == 0 && bt)
@@ -978,10 +1119,13 @@ __global__ void __launch_bounds__(kThreads, tile_waves(DP))
     const bool mask = holes || t + kTile - 1 > all_see;
     if (mask) {
       const int* entry = (const int*)table(g, kEntry) + n % kPerSegment * kTile + hf * 4;
+      uint32_t mine = 0;
+      if constexpr (TREE) mine = line.from(t - base) >> (hf * 4);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int at = (i / 4) * 8 + i % 4;
-        const bool sees = t + at + hf * 4 <= limit && !(holes && entry[at] < 0);
+        const bool up_to = TREE ? (mine >> at) & 1 : t + at + hf * 4 <= limit;
+        const bool sees = up_to && !(holes && entry[at] < 0);
         s[i] = sees ? s[i] : -INFINITY;
       }
     }
@@ -1429,13 +1573,18 @@ hipError_t launch(const void* fn, dim3 groups, size_t lds, hipStream_t s, const 
 
 template <bool BF16, int DP>
 struct Kernels {
+  template <bool TREE>
   static const void* split(int rt) {
-    if (rt == 1) return (const void*)&attend_split_kernel<BF16, DP, 1>;
-    if (rt == 2) return (const void*)&attend_split_kernel<BF16, DP, 2>;
-    if constexpr (DP < 256) return (const void*)&attend_split_kernel<BF16, DP, 4>;
+    if (rt == 1) return (const void*)&attend_split_kernel<BF16, DP, 1, TREE>;
+    if (rt == 2) return (const void*)&attend_split_kernel<BF16, DP, 2, TREE>;
+    if constexpr (DP < 256) return (const void*)&attend_split_kernel<BF16, DP, 4, TREE>;
     return nullptr;
   }
-  static const void* tile() { return (const void*)&attend_tile_kernel<BF16, DP>; }
+  static const void* split(int rt, bool tree) { return tree ? split<true>(rt) : split<false>(rt); }
+  static const void* tile(bool tree) {
+    return tree ? (const void*)&attend_tile_kernel<BF16, DP, true>
+                : (const void*)&attend_tile_kernel<BF16, DP, false>;
+  }
   static const void* join() { return (const void*)&attend_join_kernel<BF16, DP>; }
   static const void* weigh() { return (const void*)&attend_weigh_kernel<BF16, DP>; }
 };
@@ -1456,17 +1605,17 @@ const void* pick(const AttendArgs& a, F f) {
 }  // namespace
 
 hipError_t launch_attend_split(const AttendArgs& a, int rt, bool direct, hipStream_t s) {
-  const void* fn = pick(a, [&](auto k) { return decltype(k)::split(rt); });
+  const void* fn = pick(a, [&](auto k) { return decltype(k)::split(rt, a.parent != nullptr); });
   return launch(fn, dim3(a.items), split_lds(padded(a.q.D), rt, a.chunk, a.slopes != nullptr), s, a,
                 (int)direct);
 }
 
 hipError_t launch_attend_tile(const AttendArgs& a, bool direct, hipStream_t s) {
-  const void* fn = pick(a, [](auto k) { return decltype(k)::tile(); });
+  const void* fn = pick(a, [&](auto k) { return decltype(k)::tile(a.parent != nullptr); });
   const int dp = padded(a.q.D);
-  const size_t lds = dp == 64    ? TileLds<64>::kBytes
-                     : dp == 128 ? TileLds<128>::kBytes
-                                 : TileLds<256>::kBytes;
+  const size_t lds = (dp == 64    ? TileLds<64>::kBytes
+                      : dp == 128 ? TileLds<128>::kBytes
+                                  : TileLds<256>::kBytes) + (a.parent ? kMaxDrafts * 4 : 0);
   return launch(fn, dim3(a.items), lds, s, a, (int)direct);
 }
 

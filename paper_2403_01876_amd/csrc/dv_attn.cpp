@@ -1,5 +1,6 @@
 // C-ABI entry points of the 8-bit cache operators: host-side validation and
 // dispatch.  Everything is checked before the first launch.
+#include "../../include/dv_draft.h"
 #include "dv_quant_view.h"
 
 namespace {
@@ -174,8 +175,10 @@ void fill(dv::AttendArgs* a, const int32_t* q_len, const int32_t* kv_len, int64_
   a->items = (int32_t)item;
 }
 
+// `tree`: drafts that follow each other as `parent` says.
 int attend(const dv_quant* c, int32_t mb, int32_t layer, const int32_t* q_len,
-           const int32_t* kv_len, const dv_attend_args* u, void* stream) {
+           const int32_t* kv_len, bool tree, const int32_t* parent, const dv_attend_args* u,
+           void* stream) {
   Quant q;
   int rc = quant_of(c, mb, &q);
   if (rc != DV_OK) return rc;
@@ -184,15 +187,21 @@ int attend(const dv_quant* c, int32_t mb, int32_t layer, const int32_t* q_len,
   Plan p;
   rc = plan_of(q, q_len, kv_len, u, &p);
   if (rc != DV_OK) return rc;
+  if (tree && u->weigh) return DV_ERR_UNSUPPORTED;
   if (u->weigh && !q.weight) return DV_ERR_INVALID;
   int64_t tokens = 0;
-  for (int64_t b = 0; b < v.B; ++b) tokens += q_len[b];
+  for (int64_t b = 0; b < v.B; ++b) {
+    tokens += q_len[b];
+    if (tree && q_len[b] > kv_len[b]) return DV_ERR_RANGE;
+    if (tree && q_len[b] > dv::kMaxDrafts) return DV_ERR_UNSUPPORTED;
+  }
   if (u->rows < tokens) return DV_ERR_SPACE;
   if (tokens == 0) return DV_OK;
   const int64_t D = v.D;
   const int64_t strides[4] = {u->q_token, u->q_head, u->out_token, u->out_head};
   for (int64_t s : strides)
     if (s < 0 || s % 8 != 0 || s >= (1ll << 31)) return DV_ERR_INVALID;
+  if (tree && (!parent || !aligned4(parent))) return DV_ERR_INVALID;
   if (!u->q || !u->out || !aligned16(u->q) || !aligned16(u->out) || !aligned4(u->slopes) ||
       !aligned4(u->lse) || !aligned16(u->workspace))
     return DV_ERR_INVALID;
@@ -213,6 +222,9 @@ int attend(const dv_quant* c, int32_t mb, int32_t layer, const int32_t* q_len,
       overlaps(u->slopes, sn, u->out, on) || overlaps(u->slopes, sn, u->lse, ln) ||
       overlaps(u->slopes, sn, u->workspace, wn) || hits(q, u->out, on) ||
       (ln && hits(q, u->lse, ln)) || (wn && hits(q, u->workspace, wn)) ||
+      (tree && (overlaps(parent, tokens * 4, u->out, on) ||
+                overlaps(parent, tokens * 4, u->lse, ln) ||
+                overlaps(parent, tokens * 4, u->workspace, wn))) ||
       (u->weigh && (overlaps(u->q, qn, q.weight, q.slot_bytes) ||
                     overlaps(u->slopes, sn, q.weight, q.slot_bytes))))
     return DV_ERR_INVALID;
@@ -258,6 +270,7 @@ int attend(const dv_quant* c, int32_t mb, int32_t layer, const int32_t* q_len,
     a.row0 = (int32_t)row0;
     a.query = static_cast<const uint16_t*>(u->q) + row0 * u->q_token;
     a.out = static_cast<uint16_t*>(u->out) + row0 * u->out_token;
+    a.parent = tree ? parent + row0 : nullptr;
     fill(&a, q_len, kv_len, b0, nseq, G, v.H, [&](int64_t b) {
       return (q_len[b] * G + p.R - 1) / p.R * v.H * splits_of(p, kv_len[b]);
     });
@@ -325,37 +338,9 @@ int dv_quant_in(const dv_quant* dst, int32_t mb, int32_t l0, int32_t l1, const i
   const int64_t units = std::min<int64_t>(a.q.bs, longest) * v.D / 16;
   a.held = units <= 128 ? 2 : 4;
   while (a.lanes_log2 < 6 && (a.held << a.lanes_log2) < units) ++a.lanes_log2;
-  for (int32_t l = l0; l < l1; l += kLayers) {
-    const int32_t nl = std::min(kLayers, l1 - l);
-    int64_t tok = 0;
-    for (int64_t b = 0; b < v.B;) {
-      // as many sequences as fit a launch's table and grid
-      const int64_t b0 = b, first = tok;
-      int64_t items = 0;
-      int n = 0;
-      for (; b < v.B && n < kQSeqs; ++b, ++n) {
-        const int64_t s = t0 ? t0[b] : 0, e = t1[b], more = v.H * blocks_of(q, s, e);
-        if (items + more >= kMaxItems) break;
-        a.item[n] = (int32_t)items;
-        a.tok[n] = (int32_t)(tok - first);
-        a.t0[n] = (int32_t)s;
-        items += more;
-        tok += e - s;
-        if (tok - first >= (1ll << 30)) { ++b; ++n; break; }
-      }
-      a.tok[n] = (int32_t)(tok - first);
-      a.nseq = n;
-      a.b0 = (int32_t)b0;
-      a.items = (int32_t)items;
-      a.slab0 = 2 * l;
-      a.wire = static_cast<const uint8_t*>(src) + (uint64_t)(l - l0) * 2 * a.w_slab +
-               (uint64_t)first * v.H * v.D * 2;
-      if (items == 0) continue;
-      const hipError_t e = dv::launch_quant(a, 2 * nl, static_cast<hipStream_t>(stream));
-      if (e != hipSuccess) return dv::hip_fail(e, "rounding launch");
-    }
-  }
-  return DV_OK;
+  return by_launches(q, l0, l1, t0, t1, src, a, [&](int32_t nl, const QuantArgs& x) {
+    return launch_quant(x, 2 * nl, static_cast<hipStream_t>(stream));
+  });
 }
 
 int dv_attend_bytes(const dv_quant* c, const int32_t* q_len, const int32_t* kv_len,
@@ -381,7 +366,14 @@ int dv_attend_bytes(const dv_quant* c, const int32_t* q_len, const int32_t* kv_l
 
 int dv_attend(const dv_quant* c, int32_t mb, int32_t layer, const int32_t* q_len,
               const int32_t* kv_len, const dv_attend_args* a, void* stream) {
-  return attend(c, mb, layer, q_len, kv_len, a, stream);
+  return attend(c, mb, layer, q_len, kv_len, false, nullptr, a, stream);
+}
+
+int dv_attend_tree(const dv_quant* c, int32_t mb, int32_t layer, const int32_t* q_len,
+                   const int32_t* kv_len, const int32_t* parent, const dv_attend_args* a,
+                   void* stream) {
+  static_assert(dv::kMaxDrafts == DV_MAX_DRAFTS, "the interface's limit");
+  return attend(c, mb, layer, q_len, kv_len, true, parent, a, stream);
 }
 
 int dv_evict(const dv_quant* src, int32_t src_mb, const dv_quant* dst, int32_t dst_mb, int32_t l0,

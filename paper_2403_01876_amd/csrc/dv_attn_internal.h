@@ -57,6 +57,7 @@ struct AttendArgs {
   void* out;
   int64_t q_token, q_head, o_token, o_head;  // elements
   const float* slopes;
+  const int32_t* parent;  // drafts of a tree: which one each follows, else null
   float* lse;
   float* part;    // splits: [item][R rows][Dp], sums of a work item's rows
   float* ml;      // splits: [item][R rows][2], their reference and sum
@@ -75,6 +76,8 @@ struct AttendArgs {
   int32_t len[kQSeqs];        // tokens in the cache
   int32_t soff[kQSeqs];       // scores of earlier sequences, in 32 floats
 };
+// Most drafts of a sequence's tree (DV_MAX_DRAFTS of the interface).
+constexpr int kMaxDrafts = 128;
 static_assert(sizeof(AttendArgs) <= 3800, "arguments stay under 4 KB");
 // Few rows: RT tiles of 16 rows (1, 2, 4), the token axis split into chunks of
 // a.chunk tokens; `direct`: one chunk a sequence, results go straight to out.

@@ -139,4 +139,42 @@ inline int64_t blocks_of(const Quant& q, int64_t t0, int64_t t1) {
   return t1 > t0 ? (t1 + q.sb - 1) / q.sb - t0 / q.sb : 0;
 }
 
+// Tokens [t0, t1) of layers [l0, l1) of a wire at `wire`, as many layers and sequences
+// to a launch as its table and grid hold: launch(layers, a) with a's tables filled.
+template <typename Launch>
+int by_launches(const Quant& q, int32_t l0, int32_t l1, const int32_t* t0, const int32_t* t1,
+                const void* wire, QuantArgs a, Launch launch) {
+  const View& v = q.v;
+  for (int32_t l = l0; l < l1; l += kLayers) {
+    const int32_t nl = std::min(kLayers, l1 - l);
+    int64_t tok = 0;
+    for (int64_t b = 0; b < v.B;) {
+      const int64_t b0 = b, first = tok;
+      int64_t items = 0;
+      int n = 0;
+      for (; b < v.B && n < kQSeqs; ++b, ++n) {
+        const int64_t s = t0 ? t0[b] : 0, e = t1[b], more = v.H * blocks_of(q, s, e);
+        if (items + more >= kMaxItems) break;
+        a.item[n] = (int32_t)items;
+        a.tok[n] = (int32_t)(tok - first);
+        a.t0[n] = (int32_t)s;
+        items += more;
+        tok += e - s;
+        if (tok - first >= (1ll << 30)) { ++b; ++n; break; }
+      }
+      a.tok[n] = (int32_t)(tok - first);
+      a.nseq = n;
+      a.b0 = (int32_t)b0;
+      a.items = (int32_t)items;
+      a.slab0 = 2 * l;
+      a.wire = static_cast<const uint8_t*>(wire) + (uint64_t)(l - l0) * 2 * a.w_slab +
+               (uint64_t)first * v.H * v.D * 2;
+      if (items == 0) continue;
+      const hipError_t e = launch(nl, a);
+      if (e != hipSuccess) return hip_fail(e, "stream launch");
+    }
+  }
+  return DV_OK;
+}
+
 }  // namespace dv
