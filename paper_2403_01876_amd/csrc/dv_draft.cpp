@@ -14,10 +14,8 @@ using namespace dv;
 
 struct VerifyPlan {
   int64_t rows, pieces;
-  uint64_t sums, finals, turns, left, bytes;  // bytes of the workspace's parts
+  uint64_t sums, left, arrived, bytes;  // bytes of the workspace's parts
 };
-
-uint64_t up16(uint64_t n) { return (n + 15) & ~15ull; }
 
 int plan_of(const int32_t* q_len, const dv_verify_args* a, VerifyPlan* p) {
   if (!q_len || !a) return DV_ERR_INVALID;
@@ -34,10 +32,9 @@ int plan_of(const int32_t* q_len, const dv_verify_args* a, VerifyPlan* p) {
   // (a row may begin up to seven numbers after the boundary that its pieces go by)
   p->pieces = ((int64_t)a->vocab + 7 + kPiece - 1) / kPiece;
   p->sums = (uint64_t)p->rows * p->pieces * sizeof(PieceSum);
-  p->finals = (uint64_t)a->batch * sizeof(Final);
-  p->turns = up16((uint64_t)p->rows * 8);
   p->left = (uint64_t)a->batch * p->pieces * 16;
-  p->bytes = p->rows ? p->sums + p->finals + p->turns + p->left : 0;
+  p->arrived = (uint64_t)a->batch * 4;
+  p->bytes = p->rows ? p->sums + p->left + p->arrived : 0;
   if (p->bytes >= 1ull << 31) return DV_ERR_UNSUPPORTED;
   return DV_OK;
 }
@@ -95,9 +92,8 @@ int verify(const int32_t* q_len, const float* temperature, const dv_verify_args*
   a.count = u->count;
   a.next = u->next;
   a.sums = reinterpret_cast<PieceSum*>(w);
-  a.finals = p.rows ? reinterpret_cast<Final*>(w + p.sums) : nullptr;
-  a.turns = reinterpret_cast<double*>(w + p.sums + p.finals);
-  a.left = reinterpret_cast<double*>(w + p.sums + p.finals + p.turns);
+  a.left = reinterpret_cast<double*>(w + p.sums);
+  a.arrived = reinterpret_cast<int32_t*>(w + p.sums + p.left);
   a.logits_row = u->logits_row;
   a.drawn_row = u->drawn_row;
   a.vocab = u->vocab;
@@ -119,9 +115,12 @@ int verify(const int32_t* q_len, const float* temperature, const dv_verify_args*
       tok += q_len[b0 + i];
     }
     row0 += tok;
+    // Workgroups that are all on the card at once, as far as they have a piece each.
+    a.parts = (int32_t)std::min<int64_t>(p.pieces, std::max<int64_t>(1, 512 / a.nseq));
+    a.parts = (int32_t)((p.pieces + (p.pieces + a.parts - 1) / a.parts - 1) /
+                        ((p.pieces + a.parts - 1) / a.parts));  // none without a piece
     hipError_t e = tok ? launch_verify_sums(a, st) : hipSuccess;
     if (e == hipSuccess) e = launch_verify_walk(a, st);
-    if (e == hipSuccess && tok) e = launch_verify_next(a, st);
     if (e != hipSuccess) return hip_fail(e, "verification launch");
   }
   return DV_OK;

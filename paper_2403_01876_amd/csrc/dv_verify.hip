@@ -1,111 +1,155 @@
 // Which drafted tokens the target's distribution accepts, and the token after them.
 //
 // All that is decided by comparisons of sums of exponentials, and the last by where
-// a random number falls among as many of them as there are tokens: sums, and the
-// exponentials, are held in 64 bits, so that neither the order of a sum nor the last
-// bit of an exponential moves a border that anyone could tell (32 bits would, one time
-// in a few hundred over 32000 tokens).
+// a random number falls among as many of them as there are tokens.  That one takes
+// 64 bits, exponentials and sums: in 32 it would, one time in a few hundred over 32000
+// tokens, hang on the order of a sum or the last bit of an exponential.  A draft that
+// was not drawn is accepted or not by one comparison with its row's sum, for which 32
+// bits do unless the two sides lie within the sum's error of each other; then the row
+// is added up again in 64.  Drafts that were drawn leave differences of the two
+// distributions behind, whose rows are added up in 64 bits at once.
 //
-// Three launches: the sums of every row's pieces; the walk down the tree, a workgroup
-// to a sequence, from those sums and the drafts' own logits; and the last row again,
-// piece by piece, of which the workgroup that comes last finds the token.
+// Two launches.  The sums of every row's pieces, a wave to each; and a workgroup for
+// each part of a sequence's last row.  Each of these walks down the tree by itself, from
+// those sums and the drafts' own logits, adds up its part of the row that the walk
+// ends at, and the one that comes last finds the token.
 #include "dv_draft_internal.h"
 
 namespace dv {
 namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
-// 2^t for t <= 0 to 1e-14 (0 below 2^-1060, and for NaN): the nearest whole power and
-// the series of 2^f = e^(f ln 2) for the rest, |f| <= 1/2, to f^11.
+// 2^t for t of [-1020, 0] to 3e-13: the nearest whole power, which adding 1.5 * 2^52
+// leaves in the low bits, and the series of 2^f = e^(f ln 2) for the rest, |f| <= 1/2,
+// to f^10.
 struct Series {
-  double c[12];
+  double c[11];
   constexpr Series() : c{} {
     c[0] = 1;
-    for (int i = 1; i < 12; ++i) c[i] = c[i - 1] * 0.693147180559945309417232121458 / i;
+    for (int i = 1; i < 11; ++i) c[i] = c[i - 1] * 0.693147180559945309417232121458 / i;
   }
 };
 __device__ __forceinline__ double pow2(double t) {
   constexpr Series s;
-  const double n = __builtin_rint(t), f = t - n;
-  double y = s.c[11];
+  const double z = t + 0x1.8p52, f = t - (z - 0x1.8p52);
+  double y = s.c[10];
 #pragma unroll
-  for (int i = 10; i >= 0; --i) y = __builtin_fma(y, f, s.c[i]);
-  return t > -1060. ? __builtin_ldexp(y, (int)n) : 0.;
+  for (int i = 9; i >= 0; --i) y = __builtin_fma(y, f, s.c[i]);
+  return __hiloint2double(__double2hiint(y) + (__double2loint(z) << 20), __double2loint(y));
 }
 
-// A logit's share relative to the row's largest; greedy rows (scale2 0): one token's.
-// (+infinity less itself is NaN: infinite logits share all.)
-__device__ __forceinline__ double weight_of(float x, int token, float top, int arg, double scale2) {
-  if (scale2 == 0.) return token == arg ? 1. : 0.;
-  return x == top ? (x == -INFINITY ? 0. : 1.) : pow2(((double)x - top) * scale2);
-}
+// How a row's logits become shares relative to its largest, 0 below 2^-1020.
+struct Scale {
+  double scale2;  // log2(e) / temperature
+  float top;
+  int arg;        // greedy rows (scale2 0): the one token that has it all
+  // (Infinite logits share all: +infinity less itself would be NaN.)
+  __device__ __forceinline__ bool flat() const { return scale2 == 0. || top == INFINITY; }
+  __device__ __forceinline__ double flat_share(float x, int token) const {
+    return x == top && (scale2 != 0. || token == arg) ? 1. : 0.;
+  }
+  // No branches: a few of these in a row hide each other's waits.
+  __device__ __forceinline__ double share(float x) const {
+    const double t = ((double)x - top) * scale2, y = pow2(fmax(t, -1021.));
+    return t < -1020. ? 0. : y;
+  }
+  __device__ __forceinline__ double of(float x, int token) const {
+    return flat() ? flat_share(x, token) : share(x);
+  }
+};
 
 template <int TYPE>
 __device__ __forceinline__ float one_of(const void* row, int i) {
-  if constexpr (TYPE == 2) return ((const float*)row)[i];
-  const uint16_t x = ((const uint16_t*)row)[i];
-  if constexpr (TYPE == 1) return __uint_as_float((uint32_t)x << 16);
-  return (float)__builtin_bit_cast(_Float16, x);
+  float x;
+  if constexpr (TYPE == 2)
+    x = ((const float*)row)[i];
+  else if constexpr (TYPE == 1)
+    x = __uint_as_float((uint32_t)((const uint16_t*)row)[i] << 16);
+  else
+    x = (float)__builtin_bit_cast(_Float16, ((const uint16_t*)row)[i]);
+  return x == x ? x : -INFINITY;
 }
 template <int TYPE>
 __device__ __forceinline__ const void* row_of(const VerifyArgs& a, int64_t row) {
   return (const uint8_t*)a.logits + row * a.logits_row * (TYPE == 2 ? 4 : 2);
 }
-
-// Tokens to a lane, and what a lane holds of a piece: tokens first ... first + kEach - 1 of
-// a row, those outside [0, vocab) and NaN as -infinity.
-constexpr int kEach = kPiece / kThreads;
-// The token of a row's first lane: 0, or the start of its 16 bytes, which is before it.
+// Tokens of 16 bytes.
+template <int TYPE>
+constexpr int kPer = TYPE == 2 ? 4 : 8;
+// How many tokens the 16 bytes that a row begins in hold before it: a row's pieces are
+// counted from there.
 template <int TYPE>
 __device__ __forceinline__ int lead_of(const void* row) {
   return (int)((uintptr_t)row & 15) / (TYPE == 2 ? 4 : 2);
 }
+// The logits of 16 bytes; nth: NaN as -infinity.
 template <int TYPE>
-__device__ __forceinline__ void load(const void* row, int first, int vocab, float (&x)[kEach]) {
-  if (first >= 0 && first + kEach <= vocab) {
-    constexpr int kSize = TYPE == 2 ? 4 : 2, kLoads = kEach * kSize / 16, kPer = 16 / kSize;
-    const u32x4* p = (const u32x4*)((const uint8_t*)row + (int64_t)first * kSize);
-    u32x4 w[kLoads];
+__device__ __forceinline__ float raw(const u32x4& w, int i) {
+  if constexpr (TYPE == 2) return __uint_as_float(w[i]);
+  if constexpr (TYPE == 1) return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+  return (float)__builtin_bit_cast(_Float16, (uint16_t)(i & 1 ? w[i / 2] >> 16 : w[i / 2]));
+}
+template <int TYPE>
+__device__ __forceinline__ float nth(const u32x4& w, int i) {
+  return __builtin_fmaxf(raw<TYPE>(w, i), -INFINITY);
+}
+// N times 16 bytes of a row: tokens first + i * step ..., -infinity outside [0, vocab).
+template <int TYPE, int N>
+__device__ __forceinline__ void load(const void* row, int first, int step, int vocab, bool inside,
+                                     u32x4 (&w)[N]) {
+  constexpr int kSize = TYPE == 2 ? 4 : 2;
+  const uint8_t* p = (const uint8_t*)row + (int64_t)first * kSize;
+  if (inside) {  // the same in all lanes
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) w[i] = p[i];
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      if constexpr (TYPE == 2)
-        x[i] = __uint_as_float(w[i / kPer][i % kPer]);
-      else {
-        const uint32_t y = w[i / kPer][i % kPer / 2];
-        if constexpr (TYPE == 1)
-          x[i] = __uint_as_float(i & 1 ? y & 0xffff0000u : y << 16);
-        else
-          x[i] = (float)__builtin_bit_cast(_Float16, (uint16_t)(i & 1 ? y >> 16 : y));
-      }
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < kEach; ++i)
-      x[i] = first + i >= 0 && first + i < vocab ? one_of<TYPE>(row, first + i) : -INFINITY;
+    for (int i = 0; i < N; ++i) w[i] = *(const u32x4*)(p + i * step * kSize);
+    return;
   }
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) x[i] = x[i] == x[i] ? x[i] : -INFINITY;
+  for (int i = 0; i < N; ++i) {
+    const int at = first + i * step;
+    if (at >= 0 && at + kPer<TYPE> <= vocab) {
+      w[i] = *(const u32x4*)(p + i * step * kSize);
+    } else {
+#pragma unroll
+      for (int k = 0; k < kPer<TYPE>; ++k) {
+        const bool on = at + k >= 0 && at + k < vocab;
+        if constexpr (TYPE == 2) {
+          w[i][k] = on ? ((const uint32_t*)row)[at + k] : 0xff800000u;
+        } else {
+          const uint32_t x = on ? ((const uint16_t*)row)[at + k] : TYPE == 1 ? 0xff80u : 0xfc00u;
+          w[i][k / 2] = k & 1 ? w[i][k / 2] | x << 16 : x;
+        }
+      }
+    }
+  }
 }
 
 // A number of [0, 1]: NaN counts as 1.
 __device__ __forceinline__ double chance(float u) { return u < 1.f ? fmaxf(u, 0.f) : 1.; }
-__device__ __forceinline__ float some(float q) { return q > 0.f ? q : 0.f; }
+__device__ __forceinline__ float some(float q) { return q > 0.f ? fminf(q, 0x1.fffffep127f) : 0.f; }
 
-// The sum over a workgroup in a fixed order, in all of its threads (`part`: a number for
-// each wave, free again after the next barrier).
-__device__ __forceinline__ double sum_all(double x, double* part) {
-  const int waves = blockDim.x >> 6;
-#pragma unroll
-  for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
-  __syncthreads();
-  double y = part[0];
-  for (int i = 1; i < waves; ++i) y += part[i];
-  return y;
+// Sums over the lanes up to and with each one, by moves within rows of 16 and from
+// row to row: a tenth of the wait of exchanges through LDS.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double moved(double x) {  // 0 where nothing comes from
+  return __hiloint2double(
+      __builtin_amdgcn_update_dpp(0, __double2hiint(x), CTRL, ROWS, 0xf, false),
+      __builtin_amdgcn_update_dpp(0, __double2loint(x), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ double upto(double x) {
+  x += moved<0x111, 0xf>(x);  // row_shr: 1, 2, 4, 8
+  x += moved<0x112, 0xf>(x);
+  x += moved<0x114, 0xf>(x);
+  x += moved<0x118, 0xf>(x);
+  x += moved<0x142, 0xa>(x);  // row_bcast: 15 and 31
+  return x + moved<0x143, 0xc>(x);
+}
+__device__ __forceinline__ double lane_of(double x, int lane) {
+  return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(x), lane),
+                          __builtin_amdgcn_readlane(__double2loint(x), lane));
 }
 
 // The larger of two logits with their tokens, the lower token of equal ones.
@@ -117,248 +161,423 @@ __device__ __forceinline__ void larger(float& top, int& arg, float x, int i) {
 }
 
 // ---------------------------------------------------------------------------
-// A piece of a row: its largest logit, and the sum of the others' shares relative to it.
+// A piece of a row: its largest logit, and the sum of the shares relative to it; a
+// wave's.  In 32 bits (not EXACT) a share is 2^t, t = s x + c with one rounding, c = -s top;
+// c's own is the same for all and is put right in the sum.  t then errs by two half
+// steps, s's among them: 1e-5 of the smallest share that counts, and the sum of 64 lanes'
+// 64 shares by 70 half steps, 4e-6; by less than kSumError together.
 // ---------------------------------------------------------------------------
-template <int TYPE>
+constexpr double kSumError = 0x1p-15;
+
+template <int TYPE, bool EXACT>
 __global__ void __launch_bounds__(kThreads) verify_sums_kernel(VerifyArgs a) {
-  __shared__ float tops[kThreads / 64];
-  __shared__ int args[kThreads / 64];
-  __shared__ double part[kThreads / 64];
-  const int tid = threadIdx.x, l = tid & 63, wave = tid >> 6;
-  const int row = blockIdx.x / (uint32_t)a.pieces, piece = blockIdx.x - row * a.pieces;
+  constexpr int N = kPiece / 64 / kPer<TYPE>;
+  const int l = threadIdx.x & 63;
+  const int item = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6)));
+  const int row = item / (uint32_t)a.pieces, piece = item - row * a.pieces;
+  if (row >= a.tok[kQSeqs]) return;
   int below = 0;  // sequences that begin at or before this row
   for (int i = 0; i < a.nseq; i += 64)
     below += __popcll(__ballot(i + l < a.nseq && a.tok[min(i + l, a.nseq - 1)] <= row));
   const double scale2 = a.scale2[below - 1];
+  if (piece == 0 && row == a.tok[below - 1] && l == 0) a.arrived[a.b0 + below - 1] = 0;
   const void* p = row_of<TYPE>(a, a.row0 + row);
-  const int first = piece * kPiece + tid * kEach - lead_of<TYPE>(p);
-  float x[kEach];
-  load<TYPE>(p, first, a.vocab, x);
-  float top = x[0];
-  int arg = first;
+  const int start = piece * kPiece - lead_of<TYPE>(p), first = start + l * kPer<TYPE>;
+  u32x4 w[N];
+  load<TYPE>(p, first, 64 * kPer<TYPE>, a.vocab, start >= 0 && start + kPiece <= a.vocab, w);
+  float top = -INFINITY;
+  if constexpr (TYPE == 0) {
+    f16x2 most = {(_Float16)-INFINITY, (_Float16)-INFINITY};
 #pragma unroll
-  for (int i = 1; i < kEach; ++i) larger(top, arg, x[i], first + i);
+    for (int i = 0; i < N; ++i)
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) larger(top, arg, __shfl_xor(top, o), __shfl_xor(arg, o));
-  if (l == 0) {
-    tops[wave] = top;
-    args[wave] = arg;
+      for (int k = 0; k < 4; ++k) {  // NaN is left out
+        const uint32_t y = w[i][k];  // (a cast of the element itself reads the first one)
+        most = __builtin_elementwise_max(most, __builtin_bit_cast(f16x2, y));
+      }
+    top = fmaxf((float)most[0], (float)most[1]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int k = 0; k < kPer<TYPE>; ++k) top = fmaxf(top, raw<TYPE>(w[i], k));
   }
-  __syncthreads();
-  for (int i = 0; i < kThreads / 64; ++i) larger(top, arg, tops[i], args[i]);
-  double sum = 0.;
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) sum += weight_of(x[i], first + i, top, arg, scale2);
-  sum = sum_all(sum, part);
-  if (tid == 0) a.sums[((int64_t)a.row0 + row) * a.pieces + piece] = PieceSum{sum, top, arg};
+  for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+  int arg = 0;
+  double sum = 0.;
+  if (scale2 == 0. || top == INFINITY) {
+    arg = INT32_MAX;
+    int equal = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int k = 0; k < kPer<TYPE>; ++k)
+        if (nth<TYPE>(w[i], k) == top) {
+          arg = min(arg, first + i * 64 * kPer<TYPE> + k);
+          ++equal;
+        }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      arg = min(arg, __shfl_xor(arg, o));
+      equal += __shfl_xor(equal, o);
+    }
+    sum = scale2 == 0. ? 1. : equal;
+  } else if (top != -INFINITY) {
+    if constexpr (EXACT) {
+      const Scale scale{scale2, top, 0};
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int k = 0; k < kPer<TYPE>; ++k) sum += scale.share(nth<TYPE>(w[i], k));
+      sum = lane_of(upto(sum), 63);
+    } else {
+      const float s = (float)fmin(scale2, 0x1p100), c = -top * s;
+      float part = 0.f;
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int k = 0; k < kPer<TYPE>; ++k)
+          part += __builtin_amdgcn_exp2f(__builtin_fmaf(raw<TYPE>(w[i], k), s, c));
+      // Some NaN, or numbers that pass f32 on the way: each by itself.
+      if (__any(!(part < INFINITY)) || !(fabsf(c) < 0x1p100f)) {
+        part = 0.f;
+#pragma unroll 1
+        for (int u = first; u < start + kPiece; u += 64 * kPer<TYPE>)
+          for (int k = max(u, 0); k < min(u + kPer<TYPE>, a.vocab); ++k)
+            part += __builtin_amdgcn_exp2f((one_of<TYPE>(p, k) - top) * s);
+      } else {
+        part *= __builtin_amdgcn_exp2f(__builtin_fmaf(-top, s, -c));
+      }
+      sum = lane_of(upto((double)part), 63);
+    }
+  }
+  if (l == 0) a.sums[((int64_t)a.row0 + row) * a.pieces + piece] = PieceSum{sum, top, arg};
 }
 
 // ---------------------------------------------------------------------------
-// The walk: a workgroup takes a sequence.  First every draft's row is put together and
-// its token's share of the row that judges it read, all at once; then the drafts are
-// tried in order, which every thread does alike.  A draft that is rejected and was
-// drawn, with others to come that were drawn from the same distribution, takes a pass
-// over the row for the sum of what is left.
+// The walk and the last row.  First every draft's row is put together from its pieces
+// and its token's share of the row that judges it found, all at once; then the drafts
+// are tried in order, of which a wave sees with one ballot those that follow the draft
+// accepted last.  With Z the sum of what is left of a row (its shares, relative to its
+// largest logit),
+//   not drawn: a rejected token's share leaves Z,
+//   drawn: what is left of a token's share w becomes max(w - q Z, 0), whose sum takes a
+//          pass over the row where another draft is to be tried against it.
+// Then each workgroup adds up its pieces of what is left in 64 bits, and the one that
+// comes last of a sequence's finds the piece in which the random number falls, and the
+// token there.
 // ---------------------------------------------------------------------------
-constexpr int kWalkers = 1024;
+constexpr int kWalkers = 512, kWaves = kWalkers / 64;
+constexpr int kEach = kPiece / kWalkers;  // tokens of a piece that a thread takes, in order
+static_assert(kEach % 4 == 0 && kWaves <= 16, "four() tokens at a time; a row of lanes");
 
-// What r holds of token y after `turns` rejections of drawn drafts.
-__device__ __forceinline__ double after(double r, double q, const double* norms, int turns) {
-  for (int i = 0; i < turns; ++i) r = fmax(r - q, 0.) / norms[i];
-  return r;
+// The sum over the workgroup in a fixed order, in all of its threads.
+__device__ __forceinline__ double sum_all(double x, double* part) {
+  x = lane_of(upto(x), 63);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
+  __syncthreads();
+  return lane_of(upto(part[threadIdx.x & (kWaves - 1)]), kWaves - 1);
+}
+
+// Logits of tokens first ... first + 3, -infinity outside [0, vocab).
+template <int TYPE>
+__device__ __forceinline__ f32x4 four(const void* row, int first, int vocab) {
+  f32x4 x;
+  if (first >= 0 && first + 4 <= vocab) {
+    u32x4 w;
+    if constexpr (TYPE == 2) {
+      w = *(const u32x4*)((const float*)row + first);
+    } else {
+      const uint2 y = *(const uint2*)((const uint16_t*)row + first);
+      w = u32x4{y.x, y.y, 0, 0};
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = nth<TYPE>(w, i);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float y = one_of<TYPE>(row, min(max(first + i, 0), vocab - 1));
+      x[i] = first + i >= 0 && first + i < vocab ? y : -INFINITY;
+    }
+  }
+  return x;
+}
+// Probabilities of the same (of any tokens outside).
+__device__ __forceinline__ f32x4 drawn_four(const float* q, int first, int vocab) {
+  f32x4 x;
+  if (first >= 0 && first + 4 <= vocab && ((uintptr_t)(q + first) & 15) == 0) {
+    x = *(const f32x4*)(q + first);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = q[min(max(first + i, 0), vocab - 1)];
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = some(x[i]);
+  return x;
+}
+
+// What is left of a share after `turns` rejections of drawn drafts: the row held `first`
+// before the first of them, sums[i] before the i-th one after it.
+__device__ __forceinline__ double after(double w, double q, double first, const double* sums,
+                                        int turns) {
+  if (turns > 0) w = fmax(w - q * first, 0.);
+  for (int i = 1; i < turns; ++i) w = fmax(w - q * sums[i], 0.);
+  return w;
+}
+
+// Bit i of two words of drafts, the lowest taken off.
+__device__ __forceinline__ int next_of(uint64_t& lo, uint64_t& hi) {
+  const int i = lo ? __builtin_ctzll(lo) : 64 + __builtin_ctzll(hi);
+  if (lo)
+    lo &= lo - 1;
+  else
+    hi &= hi - 1;
+  return i;
 }
 
 template <int TYPE>
 __global__ void __launch_bounds__(kWalkers) verify_walk_kernel(VerifyArgs a) {
-  __shared__ double total[kMaxDrafts], share[kMaxDrafts], part[kWalkers / 64], turns[kMaxDrafts];
+  __shared__ double total[kMaxDrafts], share[kMaxDrafts], part[kWaves], parts[kWaves], sums[kMaxDrafts];
   __shared__ float top[kMaxDrafts], from[kMaxDrafts], lot[kMaxDrafts];
-  __shared__ int arg[kMaxDrafts], parent[kMaxDrafts], token[kMaxDrafts];
+  __shared__ int arg[kMaxDrafts], token[kMaxDrafts], ends[kWaves][2];
+  __shared__ bool last;
   const int tid = threadIdx.x, l = tid & 63, wave = tid >> 6;
-  const int b = blockIdx.x, tok = a.row0 + a.tok[b], nq = a.tok[b + 1] - a.tok[b];
+  const int b = blockIdx.x / (uint32_t)a.parts, at = blockIdx.x - b * a.parts;
+  const int tok = a.row0 + a.tok[b], nq = a.tok[b + 1] - a.tok[b], sb = a.b0 + b;
   const double scale2 = a.scale2[b];
   if (nq == 0) {
-    if (tid == 0) {
-      a.count[a.b0 + b] = 0;
-      if (a.finals) a.finals[a.b0 + b].rejected = -1;
-    }
+    if (tid == 0 && at == 0) a.count[sb] = 0;
     return;
   }
-  // Rows: a wave puts one together at a time.
-  for (int i = wave; i < nq; i += kWalkers / 64) {
-    const PieceSum* s = a.sums + ((int64_t)tok + i) * a.pieces;
+  // Drafts l and l + 64, in every wave: what they follow (-1: nothing, or not a token), and
+  // their tokens.
+  int up0 = -1, up1 = -1, x0 = -1, x1 = -1;
+  if (l < nq) {
+    up0 = a.parent[tok + l];
+    x0 = a.token[tok + l];
+  }
+  if (l + 64 < nq) {
+    up1 = a.parent[tok + l + 64];
+    x1 = a.token[tok + l + 64];
+  }
+  const float chance_of = tid < nq ? a.uniform[tok + tid] : 0.f;
+  // Rows: a group of lanes puts one together at a time, each its first pieces at once.
+  int lanes = 8;
+  while (lanes < 64 && lanes < a.pieces && nq * lanes * 2 <= kWalkers) lanes <<= 1;
+  for (int i0 = 0; i0 < nq; i0 += kWalkers / lanes) {
+    const int i = i0 + tid / lanes, k0 = tid & (lanes - 1);
+    const PieceSum* s = a.sums + ((int64_t)tok + min(i, nq - 1)) * a.pieces;
     float t = -INFINITY;
     int g = INT32_MAX;
+    constexpr int kHeld = 4;
+    PieceSum held[kHeld];
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) held[j] = s[min(k0 + j * lanes, a.pieces - 1)];
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) larger(t, g, held[j].top, held[j].arg);  // (or again)
+    for (int k = k0 + kHeld * lanes; k < a.pieces; k += lanes) larger(t, g, s[k].top, s[k].arg);
+    for (int o = 1; o < lanes; o <<= 1) larger(t, g, __shfl_xor(t, o), __shfl_xor(g, o));
+    const Scale scale{scale2, t, g};
+    auto of = [&](const PieceSum& x) {
+      return x.sum == 0. ? 0. : x.sum * scale.of(x.top, x.arg);
+    };
     double sum = 0.;
-    for (int k = l; k < a.pieces; k += 64) larger(t, g, s[k].top, s[k].arg);
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) larger(t, g, __shfl_xor(t, o), __shfl_xor(g, o));
-    for (int k = l; k < a.pieces; k += 64)
-      sum += scale2 == 0.      ? (s[k].arg == g ? 1. : 0.)
-             : s[k].sum == 0. ? 0.
-             : s[k].top == t  ? s[k].sum
-                              : s[k].sum * pow2(((double)s[k].top - t) * scale2);
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
-    if (l == 0) {
+    for (int j = 0; j < kHeld; ++j)
+      if (k0 + j * lanes < a.pieces) sum += of(held[j]);
+    for (int k = k0 + kHeld * lanes; k < a.pieces; k += lanes) sum += of(s[k]);
+    for (int o = 1; o < lanes; o <<= 1) sum += __shfl_xor(sum, o);
+    if (k0 == 0 && i < nq) {
       total[i] = t == -INFINITY ? 0. : sum;
       top[i] = t;
       arg[i] = g;
     }
   }
+  up0 = up0 >= 0 && up0 < l && x0 >= 0 && x0 < a.vocab ? up0 : -1;
+  up1 = up1 >= 0 && up1 < l + 64 && x1 >= 0 && x1 < a.vocab ? up1 : -1;
+  // Threads below 128 stand for a draft each.
+  const int up = wave ? up1 : up0, x = wave ? x1 : x0;
+  float y = 0.f, d = 0.f;
+  if (tid < kMaxDrafts && up >= 0) {
+    y = one_of<TYPE>(row_of<TYPE>(a, tok + up), x);
+    if (a.drawn) d = some(a.drawn[(int64_t)(tok + up) * a.drawn_row + x]);
+  }
+  __syncthreads();
   if (tid < nq) {
-    const int p = a.parent[tok + tid], x = a.token[tok + tid];
-    parent[tid] = p >= 0 && p < tid && x >= 0 && x < a.vocab ? p : -1;
+    if (up >= 0) {
+      const Scale scale{scale2, top[up], arg[up]};
+      share[tid] = total[up] == 0. ? 0. : scale.of(y, x);
+    }
+    from[tid] = d;
+    lot[tid] = chance_of;
     token[tid] = x;
-    lot[tid] = a.uniform[tok + tid];
-  }
-  __syncthreads();
-  if (tid < nq && parent[tid] >= 0) {
-    const int p = parent[tid], x = token[tid];
-    float y = one_of<TYPE>(row_of<TYPE>(a, tok + p), x);
-    y = y == y ? y : -INFINITY;
-    share[tid] = total[p] == 0. ? 0. : weight_of(y, x, top[p], arg[p], scale2);
-    from[tid] = a.drawn ? some(a.drawn[(int64_t)(tok + p) * a.drawn_row + x]) : 0.f;
   }
   __syncthreads();
 
-  int here = 0, n = 1, rejected = 0;
-  double covered = 0.;
-  bool pending = false;  // whether the last rejection's sum is not known yet
-  if (tid == 0) a.path[tok] = 0;
-  for (int i = 1; i < nq; ++i) {
-    if (parent[i] != here) continue;
-    const double u = chance(lot[i]), sum = total[here];
-    bool taken, changed = false;
-    if (sum == 0.) break;  // nothing has any probability
-    if (!a.drawn) {
-      bool again = false;
-      for (int k = 0; k < rejected; ++k) again |= (int)turns[k] == token[i];
-      const double r = again ? 0. : share[i];
-      taken = u * (sum - covered) < r;
-      if (!taken && r > 0. && sum - covered - r > 0.) {
-        covered += r;
-        changed = true;
+  const double error = a.drawn || scale2 == 0. ? 0. : scale2 > 0x1p100 ? 1. : kSumError;
+  const bool teller = tid == 0 && at == 0;
+  int here = 0, n = 1, turns = 0;
+  uint64_t gone0 = 0, gone1 = 0;  // drafts whose shares have left the row
+  bool pending = false;           // whether the last rejection's sum is not known yet
+  if (teller) a.path[tok] = 0;
+  while (total[here] != 0.) {
+    uint64_t try0 = __ballot(up0 == here), try1 = __ballot(up1 == here);
+    const void* row = row_of<TYPE>(a, tok + here);
+    const float* q = a.drawn ? a.drawn + (int64_t)(tok + here) * a.drawn_row : nullptr;
+    const Scale scale{scale2, top[here], arg[here]};
+    // The sum over the row's tokens of what is left of them.
+    auto pass = [&](int rejections) {
+      double sum = 0.;
+      const int lead = lead_of<TYPE>(row);
+#pragma unroll 1
+      for (int first = tid * 4 - lead; first < a.vocab; first += kWalkers * 4) {
+        const f32x4 z = four<TYPE>(row, first, a.vocab);
+        f32x4 d = {0, 0, 0, 0};
+        if (q) d = drawn_four(q, first, a.vocab);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum += after(scale.of(z[i], first + i), d[i], total[here], sums, rejections);
       }
-      __syncthreads();
-      if (changed && tid == 0) turns[rejected] = token[i];
-      rejected += changed;
-      __syncthreads();
-    } else {
-      if (pending) {  // the sum of what the last rejection left
-        const void* row = row_of<TYPE>(a, tok + here);
-        const float* q = a.drawn + (int64_t)(tok + here) * a.drawn_row;
-        double left = 0.;
-        for (int y = tid; y < a.vocab; y += kWalkers) {
-          float x = one_of<TYPE>(row, y);
-          x = x == x ? x : -INFINITY;
-          const double w = weight_of(x, y, top[here], arg[here], scale2) / sum, d = some(q[y]);
-          left += fmax(after(w, d, turns, rejected) - d, 0.);
+      return sum_all(sum, part);
+    };
+    double left = total[here], off = left * error;
+    int taken = -1;
+    turns = 0;
+    gone0 = gone1 = 0;
+    pending = false;
+    while (try0 | try1) {
+      const int i = next_of(try0, try1);
+      const double u = chance(lot[i]);
+      double r = share[i];
+      if (q) {
+        if (pending) {  // the sum of what the last rejection left
+          const double sum = pass(turns + 1);
+          if (sum > 0.) {
+            ++turns;
+            left = sum;
+            if (tid == 0) sums[turns] = sum;  // (the pass's barriers were after the last reads)
+            __syncthreads();
+          }
         }
-        left = sum_all(left, part);
-        __syncthreads();
-        if (left > 0. && tid == 0) turns[rejected] = left;
-        rejected += left > 0.;
-        pending = false;
-        __syncthreads();
+        pending = !(u * from[i] * left < after(r, from[i], total[here], sums, turns));
+        if (!pending) taken = i;
+      } else {
+        const int x = token[i];  // the second guess of a token has nothing left
+        if ((__ballot(up0 == here && x0 == x) & gone0) | (__ballot(up1 == here && x1 == x) & gone1))
+          r = 0.;
+        if (fabs(u * left - r) <= off || (u * left >= r && left - r <= off)) {
+          // Too near to tell, or nothing may be left: the row once more, in 64 bits.
+          const double sum = pass(0);
+          left += sum - total[here];
+          off = 0.;
+          __syncthreads();
+          if (tid == 0) total[here] = sum;
+          __syncthreads();
+        }
+        if (u * left < r) {
+          taken = i;
+        } else if (r > 0. && left - r > 0.) {
+          left -= r;
+          (i < 64 ? gone0 : gone1) |= 1ull << (i & 63);
+        }
       }
-      const double d = from[i], r = after(share[i] / sum, d, turns, rejected);
-      taken = u * d < r;
-      pending = !taken;
+      if (taken >= 0) break;
     }
-    if (taken) {
-      here = i;
-      if (tid == 0) a.path[tok + n] = i;
-      ++n;
-      rejected = 0;
-      covered = 0.;
-      pending = false;
-    }
+    if (taken < 0) break;
+    here = taken;
+    if (teller) a.path[tok + n] = here;
+    ++n;
   }
-  for (int k = tid; k < rejected; k += kWalkers) a.turns[tok + k] = turns[k];
-  if (tid == 0) {
-    a.count[a.b0 + b] = n;
-    const bool none = total[here] == 0.;
-    if (none) a.next[a.b0 + b] = -1;
-    a.finals[a.b0 + b] = Final{total[here], top[here], arg[here], tok + here,
-                               none ? -1 : 2 * rejected + pending, 0, 0};
+  if (teller) a.count[sb] = n;
+  if (total[here] == 0.) {  // nothing has any probability
+    if (teller) a.next[sb] = -1;
+    return;
   }
-}
-
-// ---------------------------------------------------------------------------
-// The last row: each workgroup adds up one piece of what is left of it, and the one that
-// comes last of a sequence's finds the piece in which the random number falls, and the
-// token there.
-// ---------------------------------------------------------------------------
-template <int TYPE>
-__global__ void __launch_bounds__(kThreads) verify_next_kernel(VerifyArgs a) {
-  __shared__ double part[kThreads / 64], scan[kThreads / 64], turns[kMaxDrafts];
-  __shared__ double found_before;
-  __shared__ int found, lowest[kThreads / 64];
-  __shared__ bool last;
-  const int tid = threadIdx.x, l = tid & 63, wave = tid >> 6;
-  const int b = blockIdx.x / (uint32_t)a.pieces, piece = blockIdx.x - b * a.pieces;
-  Final* const f = a.finals + a.b0 + b;
-  if (f->rejected < 0) return;
-  const int rejected = f->rejected >> 1, row = f->row, arg = f->arg;
-  const bool pending = f->rejected & 1;
-  const float top = f->top;
-  const double scale2 = a.scale2[b], total = f->total;
-  const int first_row = a.row0 + a.tok[b];
-  for (int k = tid; k < rejected; k += kThreads) turns[k] = a.turns[first_row + k];
-  __syncthreads();
-  const void* p = row_of<TYPE>(a, row);
-  const float* q = a.drawn ? a.drawn + (int64_t)row * a.drawn_row : nullptr;
-  const int lead = lead_of<TYPE>(p);
 
   // What this thread's tokens of a piece hold, and held before the last rejection.
+  const void* row = row_of<TYPE>(a, tok + here);
+  const float* q = a.drawn ? a.drawn + (int64_t)(tok + here) * a.drawn_row : nullptr;
+  const Scale scale{scale2, top[here], arg[here]};
+  const int lead = lead_of<TYPE>(row);
   double now[kEach], was[kEach];
+  auto sum_of = [](const double (&x)[kEach]) {
+    double y = x[0];
+#pragma unroll
+    for (int i = 1; i < kEach; ++i) y += x[i];
+    return y;
+  };
   auto weigh = [&](int piece) {
     const int first = piece * kPiece + tid * kEach - lead;
-    float x[kEach];
-    load<TYPE>(p, first, a.vocab, x);
+    float z[kEach], d[kEach];
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const int y = first + i;
-      was[i] = weight_of(x[i], y, top, arg, scale2);
-      if (y < 0 || y >= a.vocab) was[i] = 0.;
-      now[i] = was[i];
-      if (q) {
-        const double d = y >= 0 && y < a.vocab ? some(q[y]) : 0.f;
-        was[i] = after(was[i] / total, d, turns, rejected);
-        now[i] = pending ? fmax(was[i] - d, 0.) : was[i];
+    for (int i = 0; i < kEach; i += 4) {
+      const f32x4 x = four<TYPE>(row, first + i, a.vocab);
+      f32x4 y = {0, 0, 0, 0};
+      if (q) y = drawn_four(q, first + i, a.vocab);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        z[i + k] = x[k];
+        d[i + k] = y[k];
       }
     }
-    if (!q)
-      for (int k = 0; k < rejected; ++k) {
-        const int y = (int)turns[k] - first;
+    if (scale.flat()) {
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) now[i] = i == y ? 0. : now[i];
-      }
+      for (int i = 0; i < kEach; ++i) was[i] = scale.flat_share(z[i], first + i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) was[i] = scale.share(z[i]);
+    }
+    for (int k = 0; k < turns; ++k) {
+      const double by = k ? sums[k] : total[here];
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) was[i] = fmax(was[i] - d[i] * by, 0.);
+    }
+    const double by = !pending ? 0. : turns ? sums[turns] : total[here];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) now[i] = fmax(was[i] - d[i] * by, 0.);
+    for (uint64_t g = gone0, h = gone1; g | h;) {
+      const int y = token[next_of(g, h)] - first;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) now[i] = i == y ? 0. : now[i];
+    }
   };
-  weigh(piece);
-  double x = 0., y = 0.;
-#pragma unroll
-  for (int i = 0; i < kEach; ++i) {
-    x += now[i];
-    y += was[i];
+  double* const held_at = a.left + (int64_t)sb * a.pieces * 2;
+  const int per = (a.pieces + a.parts - 1) / a.parts;  // pieces of a part
+#pragma unroll 1
+  for (int piece = at * per; piece < min(a.pieces, (at + 1) * per); ++piece) {
+    weigh(piece);
+    const double x = upto(sum_of(now)), y = upto(sum_of(was));
+    __syncthreads();  // (what was in these has been read)
+    if (l == 63) {
+      part[wave] = x;
+      parts[wave] = y;
+    }
+    __syncthreads();
+    if (wave == 0) {
+      const double u = upto(part[l & (kWaves - 1)]), v = upto(parts[l & (kWaves - 1)]);
+      if (l == kWaves - 1) {
+        __hip_atomic_store(held_at + 2 * piece, u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(held_at + 2 * piece + 1, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
+    }
   }
-  x = sum_all(x, part);
-  y = sum_all(y, part);
-  double* const left = a.left + (int64_t)(a.b0 + b) * a.pieces * 2;
-  if (tid == 0) {
-    __hip_atomic_store(left + 2 * piece, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __hip_atomic_store(left + 2 * piece + 1, y, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    last = __hip_atomic_fetch_add(&f->arrived, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) ==
-           a.pieces - 1;
+  // The sums are all that one workgroup reads of another's.  They are written and read at
+  // the scope of the whole device, past each die's cache, and have arrived there (the
+  // wait) before the count goes up; a release would write every dirty line of the cache
+  // back.
+  if (tid == kWaves - 1) {  // who wrote them
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    last = __hip_atomic_fetch_add(a.arrived + sb, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+           a.parts - 1;
   }
   __syncthreads();
   if (!last) return;
-  __threadfence();
 
   // The pieces' sums, 64 at a time, in each wave alike.  What the last rejection leaves
   // counts, unless that is nothing.
   auto held = [&](int k, int which) {
-    return k < a.pieces ? __hip_atomic_load(left + 2 * k + which, __ATOMIC_RELAXED,
+    return k < a.pieces ? __hip_atomic_load(held_at + 2 * k + which, __ATOMIC_RELAXED,
                                             __HIP_MEMORY_SCOPE_AGENT)
                         : 0.;
   };
@@ -367,113 +586,83 @@ __global__ void __launch_bounds__(kThreads) verify_next_kernel(VerifyArgs a) {
     all[0] += held(k, 0);
     all[1] += held(k, 1);
   }
-#pragma unroll
-  for (int o = 32; o; o >>= 1) {
-    all[0] += __shfl_xor(all[0], o);
-    all[1] += __shfl_xor(all[1], o);
-  }
+  all[0] = lane_of(upto(all[0]), 63);
+  all[1] = lane_of(upto(all[1]), 63);
   const int which = all[0] > 0. ? 0 : 1;
-  const double goal = chance(a.uniform[first_row]) * all[which];
+  const double goal = chance(lot[0]) * all[which];
   double before = 0., sum = 0.;
-  int at = -1;  // the first piece whose sum passes the goal, or the last that holds anything
+  int place = 0;  // the first piece whose sum passes the goal, or the last that holds anything
   for (int k = 0; k < a.pieces; k += 64) {
-    const double z = held(k + l, which);
-    double up = z;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const double y = __shfl_up(up, o);
-      up += l >= o ? y : 0.;
-    }
+    const double z = held(k + l, which), up = upto(z);
     const uint64_t past = __ballot(z > 0. && sum + up > goal), any = __ballot(z > 0.);
     if (any) {
       const int i = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(any);
-      at = k + i;
-      before = sum + __shfl(up - z, i);
+      place = k + i;
+      before = sum + lane_of(up - z, i);
     }
     if (past) break;
-    sum += __shfl(up, 63);
+    sum += lane_of(up, 63);
   }
-  if (at < 0) {
-    if (tid == 0) a.next[a.b0 + b] = -1;
-    return;
-  }
-  weigh(at);
-  double mine = 0.;
+  weigh(place);
+  if (which) {
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) mine += which ? was[i] : now[i];
-  double up = mine;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const double z = __shfl_up(up, o);
-    up += l >= o ? z : 0.;
+    for (int i = 0; i < kEach; ++i) now[i] = was[i];
   }
-  if (l == 63) scan[wave] = up;
+  const double mine_here = sum_of(now), here_too = upto(mine_here);
   __syncthreads();
-  double start = before;
-  for (int i = 0; i < wave; ++i) start += scan[i];
-  start += up - mine;
-  // The first token whose sum passes the goal, in the first thread that has one; or the
-  // last that holds anything.
-  int hit = INT32_MAX, end = -1;
-  double run = start;
+  if (l == 63) part[wave] = here_too;
+  __syncthreads();
+  const double waves = upto(part[l & (kWaves - 1)]);
+  double run = before + (here_too - mine_here) + (wave ? lane_of(waves, max(wave - 1, 0)) : 0.);
+  // The first token whose sum passes the goal, or the last that holds anything.
+  int hit = -1, end = -1;
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
-    const double z = which ? was[i] : now[i];
-    const int token = at * kPiece + tid * kEach - lead + i;
-    run += z;
-    if (z > 0.) {
-      end = token;
-      if (run > goal && hit == INT32_MAX) hit = token;
+    const int y = place * kPiece - lead + tid * kEach + i;
+    run += now[i];
+    if (now[i] > 0.) {
+      end = y;
+      if (run > goal && hit < 0) hit = y;
     }
   }
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    hit = min(hit, __shfl_xor(hit, o));
-    end = max(end, __shfl_xor(end, o));
-  }
-  __syncthreads();
+  const uint64_t hits = __ballot(hit >= 0), any = __ballot(end >= 0);
   if (l == 0) {
-    lowest[wave] = hit;
-    scan[wave] = end;
+    ends[wave][0] = hits ? __builtin_amdgcn_readlane(hit, __builtin_ctzll(hits)) : -1;
+    ends[wave][1] = any ? __builtin_amdgcn_readlane(end, 63 - __builtin_clzll(any)) : -1;
   }
   __syncthreads();
-  if (tid == 0) {
-    for (int i = 1; i < kThreads / 64; ++i) {
-      hit = min(hit, lowest[i]);
-      end = max(end, (int)scan[i]);
-    }
-    a.next[a.b0 + b] = hit != INT32_MAX ? hit : end;
+  if (wave == 0) {
+    const int h = ends[l & (kWaves - 1)][0], e = ends[l & (kWaves - 1)][1];
+    const uint64_t hs = __ballot(h >= 0), es = __ballot(e >= 0 && l < kWaves);
+    if (l == (hs ? __builtin_ctzll(hs) : es ? 63 - __builtin_clzll(es) : 0)) a.next[sb] = hs ? h : e;
   }
 }
 
-template <typename F>
-hipError_t by_type(const VerifyArgs& a, F f, uint32_t groups, int threads, hipStream_t s) {
+hipError_t start(const void* fn, const VerifyArgs& a, uint32_t groups, int threads,
+                 hipStream_t s) {
   void* args[] = {const_cast<VerifyArgs*>(&a)};
-  return hipLaunchKernel(f(a.type), dim3(groups), dim3(threads), args, 0, s);
+  return hipLaunchKernel(fn, dim3(groups), dim3(threads), args, 0, s);
+}
+
+template <bool EXACT>
+const void* sums_of(int type) {
+  return type == 0   ? (const void*)&verify_sums_kernel<0, EXACT>
+         : type == 1 ? (const void*)&verify_sums_kernel<1, EXACT>
+                     : (const void*)&verify_sums_kernel<2, EXACT>;
 }
 
 }  // namespace
 
 hipError_t launch_verify_sums(const VerifyArgs& a, hipStream_t s) {
-  return by_type(a, [](int t) {
-    return t == 0   ? (const void*)&verify_sums_kernel<0>
-           : t == 1 ? (const void*)&verify_sums_kernel<1>
-                    : (const void*)&verify_sums_kernel<2>;
-  }, (uint32_t)a.tok[kQSeqs] * a.pieces, kThreads, s);
+  const uint32_t waves = (uint32_t)a.tok[kQSeqs] * a.pieces, per = kThreads / 64;
+  return start(a.drawn ? sums_of<true>(a.type) : sums_of<false>(a.type), a,
+               (waves + per - 1) / per, kThreads, s);
 }
 hipError_t launch_verify_walk(const VerifyArgs& a, hipStream_t s) {
-  return by_type(a, [](int t) {
-    return t == 0   ? (const void*)&verify_walk_kernel<0>
-           : t == 1 ? (const void*)&verify_walk_kernel<1>
-                    : (const void*)&verify_walk_kernel<2>;
-  }, (uint32_t)a.nseq, kWalkers, s);
-}
-hipError_t launch_verify_next(const VerifyArgs& a, hipStream_t s) {
-  return by_type(a, [](int t) {
-    return t == 0   ? (const void*)&verify_next_kernel<0>
-           : t == 1 ? (const void*)&verify_next_kernel<1>
-                    : (const void*)&verify_next_kernel<2>;
-  }, (uint32_t)a.nseq * a.pieces, kThreads, s);
+  return start(a.type == 0   ? (const void*)&verify_walk_kernel<0>
+               : a.type == 1 ? (const void*)&verify_walk_kernel<1>
+                             : (const void*)&verify_walk_kernel<2>,
+               a, (uint32_t)a.nseq * a.parts, kWalkers, s);
 }
 
 }  // namespace dv

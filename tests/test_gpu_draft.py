@@ -178,7 +178,7 @@ def logits_of(rows, V, rng, dtype, sharp=2.0):
 
 
 def run_verify(q_len, V, dtype, rng, *, shape="tree", drawn=False, temperature=None, pad=0,
-               logits=None, token=None, uniform=None, parent=None, q=None, broken=0.0):
+               logits=None, token=None, uniform=None, parent=None, q=None, broken=0.0, border=1e-9):
     rows, B = int(np.sum(q_len)), len(q_len)
     parent = dref.trees(q_len, rng, shape, broken) if parent is None else np.asarray(parent, np.int32)
     x = logits_of(rows, V, rng, dtype) if logits is None else logits
@@ -195,7 +195,7 @@ def run_verify(q_len, V, dtype, rng, *, shape="tree", drawn=False, temperature=N
         token = np.where(rng.random(rows) < 0.1, rng.integers(0, V, rows), token)
     u = rng.random(rows).astype(np.float32) if uniform is None else np.asarray(uniform, np.float32)
     want = dref.verify(q_len, parent, token, near, u, temperature, q if drawn else None)
-    if want[3] < 1e-9:
+    if want[3] < border:
         pytest.skip("a decision at its border")
     store = torch.full((rows + 2, V + pad), 50.0, dtype=dtype)
     store[:rows, :V] = x
@@ -272,6 +272,31 @@ def test_verify_greedy_takes_the_lowest_of_equal_logits():
     got = run_verify([4], 9000, torch.bfloat16, rng, shape="chain", logits=x, token=[0, 77, 77, 4100],
                      temperature=np.zeros(1, np.float32))
     assert got[1].tolist() == [3] and got[2].tolist() == [77]
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_verify_next_to_the_border(dtype):
+    """Random numbers as near to the probability that decides as 32 bits come, on either side:
+    about 1e-8 of it, where sums in 32 bits would not tell.  (5000 shares, each to 3e-13, and
+    as many roundings of 1e-16 stay below 1e-12.)"""
+    rng = np.random.default_rng(7)
+    V = 5000
+    for k in range(12):
+        x = logits_of(6, V, rng, TYPES[dtype])
+        p = dref.target(x[0].double().numpy(), 1.0)
+        token = np.argsort(-p)[:6]
+        r, u = p.copy(), np.full(6, 0.37, np.float32)
+        for i in range(1, 6):  # each rejected at its border, the last accepted
+            u[i] = np.float32(r[token[i]])
+            if i < 5 and float(u[i]) < r[token[i]]:
+                u[i] = np.nextafter(u[i], np.float32(1))
+            if i == 5 and float(u[i]) >= r[token[i]]:
+                u[i] = np.nextafter(u[i], np.float32(0))
+            r[token[i]] = 0
+            r /= r.sum()
+        got = run_verify([6], V, TYPES[dtype], rng, shape="star", logits=x, token=token, uniform=u,
+                         temperature=np.ones(1, np.float32), border=1e-12)
+        assert got[0].tolist()[:2] == [0, 5]
 
 
 def test_verify_special_logits():
