@@ -112,6 +112,30 @@ struct Seq {
   int b, k;           // index in the launch; the item's index in the sequence
   int len, tok, nq;   // tokens in the cache; queries of earlier sequences; its own
 };
+// Trees, whose sequences stand in another order than the batch's (AttendArgs): b is the
+// index in the batch's order.
+__device__ __forceinline__ Seq tree_seq_of(const AttendArgs& a, int item) {
+  const int lane = threadIdx.x & 63;
+  const int first = a.item[lane], len = a.len[lane], t0 = a.tok[lane], id = a.soff[lane];
+  Seq q;
+  int i = __popcll(__ballot(first <= item)) - 1, word;
+  if (i == 63 && a.nseq > 64) {
+    for (int k = 64; k < a.nseq; k += 64) i += __popcll(__ballot(a.item[k + lane] <= item));
+    i = __builtin_amdgcn_readfirstlane(i);
+    q.k = item - a.item[i];
+    q.len = a.len[i];
+    q.tok = a.tok[i];
+    word = a.soff[i];
+  } else {
+    q.k = item - __builtin_amdgcn_readlane(first, i);
+    q.len = __builtin_amdgcn_readlane(len, i);
+    q.tok = __builtin_amdgcn_readlane(t0, i);
+    word = __builtin_amdgcn_readlane(id, i);
+  }
+  q.nq = word & 255;
+  q.b = word >> 8;
+  return q;
+}
 __device__ __forceinline__ Seq seq_of(const AttendArgs& a, int item) {
   const int lane = threadIdx.x & 63;
   const int first = a.item[lane], len = a.len[lane], t0 = a.tok[lane], t1 = a.tok[lane + 1];
@@ -409,7 +433,7 @@ __global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
   const int item = blockIdx.x;
-  const Seq seq = seq_of(a, item);
+  const Seq seq = TREE ? tree_seq_of(a, item) : seq_of(a, item);
   const int b = seq.b, sb = a.b0 + b, len = seq.len, nq = seq.nq, rows = nq * a.G;
   const int nsplit = max(1, scalar((len + a.chunk - 1) / a.chunk));
   const int h = scalar(seq.k / nsplit), c0 = (seq.k - h * nsplit) * a.chunk;
@@ -864,7 +888,7 @@ __global__ void __launch_bounds__(kThreads, tile_waves(DP))
   const int wave = scalar(tid >> 6);
 
   const int item = blockIdx.x;
-  const Seq seq = seq_of(a, item);
+  const Seq seq = TREE ? tree_seq_of(a, item) : seq_of(a, item);
   const int b = seq.b, sb = a.b0 + b, len = seq.len, nq = seq.nq, rows = nq * a.G;
   const int nsplit = max(1, scalar((len + a.chunk - 1) / a.chunk));
   const int tiles = (rows + kTileRows - 1) / kTileRows;
@@ -1041,6 +1065,7 @@ __global__ void __launch_bounds__(kThreads, tile_waves(DP))
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
   float m = kLow, sum = 0.f;
+  const bool idle = r0 + wave * 32 >= rows;
   bool scaled = a.slopes != nullptr;  // whether scores get their factor by themselves
   auto key = [&](int n, int e) {
     return *(const u32x4*)(lds + L::kKeys + (n & 1) * L::kBuf + c * kPitch + e * 32 + hf * 16);
@@ -1100,6 +1125,17 @@ __global__ void __launch_bounds__(kThreads, tile_waves(DP))
       }
     }
     fetch(n + kAhead, N - 1);
+    // A wave without rows has only the codes to do.  (200 rows in two tiles, 131071 tokens:
+    // 187 us a call, with its products 190.)
+    if (TREE && idle) {
+      wait_loads<2 * UT>();
+#pragma unroll
+      for (int i = 0; i < UT; ++i)
+        put(take(i, tile_of(i, n), holes_at(tile_of(i, n), n)), i, tile_of(i, n),
+            holes_at(tile_of(i, n), n));
+      lds_barrier();
+      continue;
+    }
     u32x4 y[KS];
 #pragma unroll
     for (int e = 0; e < KS; ++e) y[e] = key(n + 1, e);
@@ -1163,6 +1199,9 @@ __global__ void __launch_bounds__(kThreads, tile_waves(DP))
     u32x4 p[2], v[DB];  // p: 16 tokens each, slots hf * 8 + 0..7 of the inner axis
 #pragma unroll
     for (int i = 0; i < 16; ++i) z[i] = 0.f;
+    // (Of two waves the one in its products goes first, and the other's exponentials find
+    // the matrix unit busy: 32 x 40 to 64 drafts 189 us a call, without this 196.)
+    if (TREE) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int e = 0; e < KS; ++e) {
       z = T::mma32(y[e], qr[e], z);
@@ -1196,6 +1235,7 @@ __global__ void __launch_bounds__(kThreads, tile_waves(DP))
       put(raws[i], i, tile_of(i, n), holes_at(tile_of(i, n), n));
 #pragma unroll
     for (int d = 0; d < DB; ++d) o[d] = T::mma32(v[d], p[1], o[d]);
+    if (TREE) __builtin_amdgcn_s_setprio(0);
     settle(z);
     s = z;
     lds_barrier();
@@ -1275,7 +1315,7 @@ __global__ void __launch_bounds__(kThreads) attend_join_kernel(AttendArgs a, int
   const QLayout& q = a.q;
   const int tid = threadIdx.x;
   const int item = blockIdx.x;
-  const Seq seq = seq_of(a, item);
+  const Seq seq = a.parent ? tree_seq_of(a, item) : seq_of(a, item);
   const int b = seq.b, sb = a.b0 + b, len = seq.len, nq = seq.nq, rows = nq * a.G;
   const int nsplit = max(1, scalar((len + a.chunk - 1) / a.chunk));
   const int tiles = scalar((rows + R - 1) / R);

@@ -75,6 +75,8 @@ struct AttendArgs {
   int32_t tok[kQSeqs + 1];    // queries of earlier sequences
   int32_t len[kQSeqs];        // tokens in the cache
   int32_t soff[kQSeqs];       // scores of earlier sequences, in 32 floats
+  // Trees: the longest sequences first; tok[i] is the first row of the i-th and soff[i]
+  // 256 times its index in the batch's order plus its drafts.
 };
 // Most drafts of a sequence's tree (DV_MAX_DRAFTS of the interface).
 constexpr int kMaxDrafts = 128;

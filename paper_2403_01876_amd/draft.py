@@ -48,7 +48,7 @@ for _name, _args in {
     _f.restype = ctypes.c_int
 
 
-def _array(name: str, x, dtype, least: int):
+def _array(name: str, x, dtype, least: int = 0):
     """The address of a contiguous device tensor of at least so many numbers."""
     if x.dtype is not dtype or not x.is_contiguous() or x.numel() < least:
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of {least} numbers or more, "
@@ -57,10 +57,20 @@ def _array(name: str, x, dtype, least: int):
 
 
 def _lengths(name: str, x):
-    a = np.ascontiguousarray(x, dtype=np.int32)
-    if a.ndim != 1:
+    """One-dimensional int32 lengths: the array, its address and size."""
+    n = len(x)
+    a, p = _i32(x, n)
+    if a.ndim != 1 or a.size != n:
         raise ValueError(f"{name} must be one-dimensional, got {a.shape}")
-    return a
+    return a, p, n
+
+
+def _temperatures(t, batch: int):
+    """float32, one for each sequence."""
+    if type(t) is not np.ndarray or t.dtype != np.float32 or t.shape != (batch,) or \
+            not t.flags.c_contiguous:
+        t = np.ascontiguousarray(np.broadcast_to(np.asarray(t, dtype=np.float32), (batch,)))
+    return t
 
 
 def dv_attend_tree(c: QuantCache, mb: int, layer: int, q_len, kv_len, parent, q, out,
@@ -72,14 +82,15 @@ def dv_attend_tree(c: QuantCache, mb: int, layer: int, q_len, kv_len, parent, q,
     a0, p0 = _i32(q_len, cache.batch)
     a1, p1 = _i32(kv_len, cache.batch)
     a = _attend_args(c, q, out, scale, slopes, None, lse, workspace)
-    parent = _array("parent", parent, torch.int32, 0 if a0 is None else int(a0.sum()))
-    rc = lib.dv_attend_tree(c.ref, mb, layer, p0, p1, parent, ctypes.byref(a), _stream(stream))
+    at = _array("parent", parent, torch.int32)
+    a.rows = min(a.rows, parent.numel())
+    rc = lib.dv_attend_tree(c.ref, mb, layer, p0, p1, at, ctypes.byref(a), _stream(stream))
     return _check(rc, "dv_attend_tree", check)
 
 
 def _table(name: str, x, types):
     if x.dim() != 2 or x.dtype not in types or (x.shape[1] > 1 and x.stride(1) != 1):
-        raise ValueError(f"{name} must be a tensor [drafts, vocab] of {types} with contiguous "
+        raise ValueError(f"{name} must be a tensor [drafts, vocab] of {tuple(types)} with contiguous "
                          f"rows, got {tuple(x.shape)} {x.dtype}")
     # (one row may have any stride)
     return x.data_ptr(), max(x.stride(0), x.shape[1]) if x.shape[0] < 2 else x.stride(0)
@@ -88,12 +99,12 @@ def _table(name: str, x, types):
 def dv_verify_bytes(q_len, logits, drawn: bool = False, check: bool = True):
     """Workspace bytes of a dv_verify with these lengths and logits' shape; ``drawn``:
     whether it will be given the drafts' distributions."""
-    n = _lengths("q_len", q_len)
-    _table("logits", logits, tuple(_TYPES))
-    a = dv_verify_args(type=_TYPES[logits.dtype], batch=len(n), vocab=logits.shape[1],
+    n, p, batch = _lengths("q_len", q_len)
+    _table("logits", logits, _TYPES)
+    a = dv_verify_args(type=_TYPES[logits.dtype], batch=batch, vocab=logits.shape[1],
                        drawn=16 if drawn else None)
     out = _u64(0)
-    rc = lib.dv_verify_bytes(n.ctypes.data, ctypes.byref(a), ctypes.byref(out))
+    rc = lib.dv_verify_bytes(p, ctypes.byref(a), ctypes.byref(out))
     _check(rc, "dv_verify_bytes", check)
     return out.value if check else (rc, out.value)
 
@@ -106,33 +117,32 @@ def dv_verify(q_len, parent, token, logits, uniform, path, count, next, temperat
     which follow them were drawn from.  ``path`` (int32 [drafts]), ``count`` and ``next`` (int32
     [batch]) receive the result.  ``temperature``: a number for all, or one for each sequence
     (host); ``workspace``: a tensor of dv_verify_bytes bytes."""
-    n = _lengths("q_len", q_len)
-    rows, batch = int(n.sum()), len(n)
-    la, lr = _table("logits", logits, tuple(_TYPES))
-    have = logits.shape[0]
+    n, p, batch = _lengths("q_len", q_len)
+    la, lr = _table("logits", logits, _TYPES)
+    rows, vocab = logits.shape
     da = dr = 0
     if drawn is not None:
         da, dr = _table("drawn", drawn, (torch.float32,))
-        if drawn.shape[1] != logits.shape[1]:
+        if drawn.shape[1] != vocab:
             raise ValueError(f"logits {tuple(logits.shape)}, drawn {tuple(drawn.shape)}")
-        have = min(have, drawn.shape[0])
-    t = None
+        rows = min(rows, drawn.shape[0])
+    rows = min(rows, parent.numel(), token.numel(), uniform.numel(), path.numel())
+    ta = None
     if temperature is not None:
-        t = np.ascontiguousarray(np.broadcast_to(np.asarray(temperature, dtype=np.float32), (batch,)))
+        t = _temperatures(temperature, batch)
+        ta = t.ctypes.data
     wb = 0
     if workspace is not None:
         if not workspace.is_contiguous():
             raise ValueError(f"workspace must be contiguous, got strides {workspace.stride()}")
         wb = workspace.numel() * workspace.element_size()
-    a = dv_verify_args(_TYPES[logits.dtype], batch, logits.shape[1], have, la, lr, da, dr,
-                       _array("parent", parent, torch.int32, rows),
-                       _array("token", token, torch.int32, rows),
-                       _array("uniform", uniform, torch.float32, rows),
-                       _array("path", path, torch.int32, rows),
-                       _array("count", count, torch.int32, batch),
-                       _array("next", next, torch.int32, batch), _addr(workspace), wb)
-    rc = lib.dv_verify(n.ctypes.data, None if t is None else t.ctypes.data, ctypes.byref(a),
-                       _stream(stream))
+    i32 = torch.int32
+    a = dv_verify_args(_TYPES[logits.dtype], batch, vocab, rows, la, lr, da, dr,
+                       _array("parent", parent, i32), _array("token", token, i32),
+                       _array("uniform", uniform, torch.float32), _array("path", path, i32),
+                       _array("count", count, i32, batch), _array("next", next, i32, batch),
+                       _addr(workspace), wb)
+    rc = lib.dv_verify(p, ta, ctypes.byref(a), _stream(stream))
     return _check(rc, "dv_verify", check)
 
 
@@ -143,7 +153,7 @@ def dv_keep_path(c: QuantCache, mb: int, l0: int, l1: int, q_len, kv_len, path, 
     batch = c.cache.c.batch
     a0, p0 = _i32(q_len, batch)
     a1, p1 = _i32(kv_len, batch)
-    path = _array("path", path, torch.int32, 0 if a0 is None else int(a0.sum()))
+    path = _array("path", path, torch.int32, 0 if a0 is None else sum(a0.tolist()))
     count = _array("count", count, torch.int32, batch)
     rc = lib.dv_keep_path(c.ref, mb, l0, l1, p0, p1, path, count, _stream(stream))
     return _check(rc, "dv_keep_path", check)

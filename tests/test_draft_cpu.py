@@ -195,9 +195,11 @@ def test_binding_refusals():
     qc = attn.QuantCache(c, [SCALE], scale_block=16)
     q = torch.zeros((2, 4, 64), dtype=torch.float16)
     parent = torch.zeros(2, dtype=torch.int32)
-    for bad in (parent.long(), parent[:1], torch.zeros(4, dtype=torch.int32)[::2]):
+    for bad in (parent.long(), torch.zeros(4, dtype=torch.int32)[::2]):
         with pytest.raises(ValueError, match="parent must be"):
             draft.dv_attend_tree(qc, 0, 0, [2], [4], bad, q, q.clone(), 1.0)
+    with pytest.raises(dv.DvError):  # too few
+        draft.dv_attend_tree(qc, 0, 0, [2], [4], parent[:1], q, q.clone(), 1.0)
     with pytest.raises(ValueError, match="q must be"):
         draft.dv_attend_tree(qc, 0, 0, [2], [4], parent, q[0], q.clone(), 1.0)
     with pytest.raises(dv.DvError):
@@ -207,16 +209,18 @@ def test_binding_refusals():
     good = dict(q_len=[2], parent=parent, token=parent.clone(), logits=logits, uniform=u,
                 path=parent.clone(), count=one, next=one.clone())
     for k, bad in (("logits", logits.double()), ("logits", logits.t()), ("uniform", u.double()),
-                   ("token", parent.long()), ("path", parent[:1]), ("count", u),
-                   ("next", torch.zeros(0, dtype=torch.int32)), ("q_len", [[2]]),
+                   ("token", parent.long()), ("path", parent.short()), ("count", u),
+                   ("next", torch.zeros(0, dtype=torch.int32)), ("q_len", [[2, 0]]),
                    ("drawn", logits.half()), ("drawn", logits[:, :40]),
                    ("workspace", torch.zeros((8, 8))[:, :4]), ("temperature", [1.0, 1.0])):
         with pytest.raises(ValueError):
             draft.dv_verify(**{**good, k: bad})
     with pytest.raises(dv.DvError):  # no workspace
         draft.dv_verify(**good)
-    with pytest.raises(dv.DvError):  # more drafts than rows
-        draft.dv_verify(**{**good, "logits": logits[:1]})
+    room = torch.zeros(1 << 16, dtype=torch.uint8)
+    for k in ("logits", "path", "parent", "token", "uniform"):  # more drafts than rows
+        with pytest.raises(dv.DvError, match="SPACE|space|capacity|-3|small"):
+            draft.dv_verify(**{**good, k: good[k][:1], "workspace": room})
     with pytest.raises(ValueError, match="path must be"):
         draft.dv_keep_path(qc, 0, 0, 1, [2], [4], parent[:1], one)
 
