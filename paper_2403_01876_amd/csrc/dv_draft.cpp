@@ -172,7 +172,7 @@ int dv_keep_path(const dv_quant* c, int32_t mb, int32_t l0, int32_t l1, const in
   const int64_t seqs = std::min<int64_t>(kQSeqs, kMaxItems / v.H);
   for (int32_t l = l0; l < l1; l += kLayers) {
     const int32_t nl = std::min(kLayers, l1 - l);
-    a.slab0 = 2 * l;
+    a.l0 = l;
     int64_t row0 = 0;
     for (int64_t b0 = 0; b0 < v.B; b0 += seqs) {
       a.b0 = (int32_t)b0;
@@ -188,7 +188,7 @@ int dv_keep_path(const dv_quant* c, int32_t mb, int32_t l0, int32_t l1, const in
       a.tok[a.nseq] = tok;
       row0 += tok;
       if (tok == 0) continue;
-      const hipError_t e = launch_keep(a, 2 * nl, static_cast<hipStream_t>(stream));
+      const hipError_t e = launch_keep(a, nl, static_cast<hipStream_t>(stream));
       if (e != hipSuccess) return hip_fail(e, "path launch");
     }
   }

@@ -41,18 +41,18 @@ hipError_t launch_verify_sums(const VerifyArgs& a, hipStream_t s);
 hipError_t launch_verify_walk(const VerifyArgs& a, hipStream_t s);
 
 // ---- dv_keep_path ----
-// A wave takes one head of one sequence in one slab.
+// A wave takes one head of one sequence in one layer.
 struct KeepArgs {
   QLayout q;
   const int32_t* path;   // advanced to this launch's first row
   const int32_t* count;  // and sequence
-  int32_t slab0, b0, nseq;
+  int32_t l0, b0, nseq;
   FastDiv d_du, d_heads;
   int32_t base[kQSeqs];
   int32_t tok[kQSeqs + 1];  // rows of earlier sequences
 };
 static_assert(sizeof(KeepArgs) <= 3584, "arguments stay under 4 KB");
-hipError_t launch_keep(const KeepArgs& a, uint32_t nslabs, hipStream_t s);
+hipError_t launch_keep(const KeepArgs& a, uint32_t layers, hipStream_t s);
 
 // ---- dv_quant_out ----
 // Work items as of dv_quant_in; `held` 8-code units to a lane at a time.
