@@ -165,7 +165,7 @@ __device__ __forceinline__ void larger(float& top, int& arg, float x, int i) {
 // wave's.  In 32 bits (not EXACT) a share is 2^t, t = s x + c with one rounding, c = -s top;
 // c's own is the same for all and is put right in the sum.  t then errs by two half
 // steps, s's among them: 1e-5 of the smallest share that counts, and the sum of 64 lanes'
-// 64 shares by 70 half steps, 4e-6; by less than kSumError together.
+// 32 shares by 40 half steps, 3e-6; by less than kSumError together.
 // ---------------------------------------------------------------------------
 constexpr double kSumError = 0x1p-15;
 
@@ -180,7 +180,14 @@ __global__ void __launch_bounds__(kThreads) verify_sums_kernel(VerifyArgs a) {
   for (int i = 0; i < a.nseq; i += 64)
     below += __popcll(__ballot(i + l < a.nseq && a.tok[min(i + l, a.nseq - 1)] <= row));
   const double scale2 = a.scale2[below - 1];
-  if (piece == 0 && row == a.tok[below - 1] && l == 0) a.arrived[a.b0 + below - 1] = 0;
+  const int first_row = a.tok[below - 1], draft = row - first_row;
+  if (piece == 0 && draft == 0 && l == 0) a.arrived[a.b0 + below - 1] = 0;
+  if (!EXACT) {  // a row that no other draft follows judges none
+    const int nq = a.tok[below] - first_row;
+    const int32_t* parent = a.parent + a.row0 + first_row;
+    const int up0 = l < nq ? parent[l] : -1, up1 = l + 64 < nq ? parent[l + 64] : -1;
+    if (!__any(up0 == draft || up1 == draft)) return;
+  }
   const void* p = row_of<TYPE>(a, a.row0 + row);
   const int start = piece * kPiece - lead_of<TYPE>(p), first = start + l * kPer<TYPE>;
   u32x4 w[N];
@@ -340,8 +347,9 @@ __device__ __forceinline__ int next_of(uint64_t& lo, uint64_t& hi) {
 template <int TYPE>
 __global__ void __launch_bounds__(kWalkers) verify_walk_kernel(VerifyArgs a) {
   __shared__ double total[kMaxDrafts], share[kMaxDrafts], part[kWaves], parts[kWaves], sums[kMaxDrafts];
+  __shared__ float tops[kWaves];
   __shared__ float top[kMaxDrafts], from[kMaxDrafts], lot[kMaxDrafts];
-  __shared__ int arg[kMaxDrafts], token[kMaxDrafts], ends[kWaves][2];
+  __shared__ int arg[kMaxDrafts], token[kMaxDrafts], judges[kMaxDrafts], ends[kWaves][2];
   __shared__ bool last;
   const int tid = threadIdx.x, l = tid & 63, wave = tid >> 6;
   const int b = blockIdx.x / (uint32_t)a.parts, at = blockIdx.x - b * a.parts;
@@ -362,6 +370,7 @@ __global__ void __launch_bounds__(kWalkers) verify_walk_kernel(VerifyArgs a) {
     up1 = a.parent[tok + l + 64];
     x1 = a.token[tok + l + 64];
   }
+  if (tid < kMaxDrafts) judges[tid] = a.drawn != nullptr;
   const float chance_of = tid < nq ? a.uniform[tok + tid] : 0.f;
   // Rows: a group of lanes puts one together at a time, each its first pieces at once.
   int lanes = 8;
@@ -397,6 +406,10 @@ __global__ void __launch_bounds__(kWalkers) verify_walk_kernel(VerifyArgs a) {
   }
   up0 = up0 >= 0 && up0 < l && x0 >= 0 && x0 < a.vocab ? up0 : -1;
   up1 = up1 >= 0 && up1 < l + 64 && x1 >= 0 && x1 < a.vocab ? up1 : -1;
+  // Rows that a draft follows; of the others there are no sums where drafts were not drawn.
+  __syncthreads();  // (cleared)
+  if (wave == 0 && up0 >= 0) judges[up0] = 1;
+  if (wave == 0 && up1 >= 0) judges[up1] = 1;
   // Threads below 128 stand for a draft each.
   const int up = wave ? up1 : up0, x = wave ? x1 : x0;
   float y = 0.f, d = 0.f;
@@ -422,7 +435,7 @@ __global__ void __launch_bounds__(kWalkers) verify_walk_kernel(VerifyArgs a) {
   uint64_t gone0 = 0, gone1 = 0;  // drafts whose shares have left the row
   bool pending = false;           // whether the last rejection's sum is not known yet
   if (teller) a.path[tok] = 0;
-  while (total[here] != 0.) {
+  while (judges[here] && total[here] != 0.) {
     uint64_t try0 = __ballot(up0 == here), try1 = __ballot(up1 == here);
     const void* row = row_of<TYPE>(a, tok + here);
     const float* q = a.drawn ? a.drawn + (int64_t)(tok + here) * a.drawn_row : nullptr;
@@ -443,9 +456,6 @@ __global__ void __launch_bounds__(kWalkers) verify_walk_kernel(VerifyArgs a) {
     };
     double left = total[here], off = left * error;
     int taken = -1;
-    turns = 0;
-    gone0 = gone1 = 0;
-    pending = false;
     while (try0 | try1) {
       const int i = next_of(try0, try1);
       const double u = chance(lot[i]);
@@ -486,11 +496,15 @@ __global__ void __launch_bounds__(kWalkers) verify_walk_kernel(VerifyArgs a) {
     }
     if (taken < 0) break;
     here = taken;
+    turns = 0;
+    gone0 = gone1 = 0;
+    pending = false;
     if (teller) a.path[tok + n] = here;
     ++n;
   }
   if (teller) a.count[sb] = n;
-  if (total[here] == 0.) {  // nothing has any probability
+  const bool bare = !judges[here];  // a row without sums: what is left of it is all of it
+  if (!bare && total[here] == 0.) {  // nothing has any probability
     if (teller) a.next[sb] = -1;
     return;
   }
@@ -498,7 +512,7 @@ __global__ void __launch_bounds__(kWalkers) verify_walk_kernel(VerifyArgs a) {
   // What this thread's tokens of a piece hold, and held before the last rejection.
   const void* row = row_of<TYPE>(a, tok + here);
   const float* q = a.drawn ? a.drawn + (int64_t)(tok + here) * a.drawn_row : nullptr;
-  const Scale scale{scale2, top[here], arg[here]};
+  Scale scale{scale2, top[here], arg[here]};
   const int lead = lead_of<TYPE>(row);
   double now[kEach], was[kEach];
   auto sum_of = [](const double (&x)[kEach]) {
@@ -507,7 +521,7 @@ __global__ void __launch_bounds__(kWalkers) verify_walk_kernel(VerifyArgs a) {
     for (int i = 1; i < kEach; ++i) y += x[i];
     return y;
   };
-  auto weigh = [&](int piece) {
+  auto weigh = [&](int piece, bool alone) {
     const int first = piece * kPiece + tid * kEach - lead;
     float z[kEach], d[kEach];
 #pragma unroll
@@ -520,6 +534,26 @@ __global__ void __launch_bounds__(kWalkers) verify_walk_kernel(VerifyArgs a) {
         z[i + k] = x[k];
         d[i + k] = y[k];
       }
+    }
+    if (alone) {  // shares relative to the piece's own largest logit
+      float big = z[0];
+      int at = first;
+#pragma unroll
+      for (int i = 1; i < kEach; ++i) larger(big, at, z[i], first + i);
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) larger(big, at, __shfl_xor(big, o), __shfl_xor(at, o));
+      __syncthreads();
+      if (l == 0) {
+        tops[wave] = big;
+        ends[wave][0] = at;
+      }
+      __syncthreads();
+      big = tops[0];
+      at = ends[0][0];
+#pragma unroll
+      for (int i = 1; i < kWaves; ++i) larger(big, at, tops[i], ends[i][0]);
+      scale.top = big;
+      scale.arg = at;
     }
     if (scale.flat()) {
 #pragma unroll
@@ -546,8 +580,10 @@ __global__ void __launch_bounds__(kWalkers) verify_walk_kernel(VerifyArgs a) {
   const int per = (a.pieces + a.parts - 1) / a.parts;  // pieces of a part
 #pragma unroll 1
   for (int piece = at * per; piece < min(a.pieces, (at + 1) * per); ++piece) {
-    weigh(piece);
-    const double x = upto(sum_of(now)), y = upto(sum_of(was));
+    weigh(piece, bare);
+    double x = upto(sum_of(now));
+    const double y = upto(sum_of(was));
+    if (bare && scale.top == -INFINITY) x = 0.;
     __syncthreads();  // (what was in these has been read)
     if (l == 63) {
       part[wave] = x;
@@ -555,7 +591,8 @@ __global__ void __launch_bounds__(kWalkers) verify_walk_kernel(VerifyArgs a) {
     }
     __syncthreads();
     if (wave == 0) {
-      const double u = upto(part[l & (kWaves - 1)]), v = upto(parts[l & (kWaves - 1)]);
+      const double u = upto(part[l & (kWaves - 1)]);
+      const double v = bare ? (double)scale.top : upto(parts[l & (kWaves - 1)]);
       if (l == kWaves - 1) {
         __hip_atomic_store(held_at + 2 * piece, u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         __hip_atomic_store(held_at + 2 * piece + 1, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -581,19 +618,44 @@ __global__ void __launch_bounds__(kWalkers) verify_walk_kernel(VerifyArgs a) {
                                             __HIP_MEMORY_SCOPE_AGENT)
                         : 0.;
   };
-  double all[2] = {0., 0.};
-  for (int k = l; k < a.pieces; k += 64) {
-    all[0] += held(k, 0);
-    all[1] += held(k, 1);
+  int which = 0;
+  double all = 0.;
+  if (bare) {  // the row's largest logit, which shares are relative to from here on
+    float big = -INFINITY;
+    for (int k = l; k < a.pieces; k += 64) big = fmaxf(big, (float)held(k, 1));
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) big = fmaxf(big, __shfl_xor(big, o));
+    scale.top = big;
+    if (big == -INFINITY) {  // nothing has any probability
+      if (tid == 0) a.next[sb] = -1;
+      return;
+    }
   }
-  all[0] = lane_of(upto(all[0]), 63);
-  all[1] = lane_of(upto(all[1]), 63);
-  const int which = all[0] > 0. ? 0 : 1;
-  const double goal = chance(lot[0]) * all[which];
+  bool found = false;  // greedy: the first piece that has the largest logit is all there is
+  auto amount = [&](int k) {
+    const double x = held(k, which);
+    if (!bare) return x;
+    const double y = x == 0. ? 0. : x * scale.of((float)held(k, 1), scale.arg);
+    if (scale2 != 0.) return y;
+    const uint64_t have = __ballot(k < a.pieces && x != 0. && (float)held(k, 1) == scale.top);
+    const bool mine = have && !found && l == __builtin_ctzll(have);
+    found |= have != 0;
+    return mine ? 1. : 0.;
+  };
+  for (int k = l; k < a.pieces + l; k += 64) all += amount(k);
+  all = lane_of(upto(all), 63);
+  if (!bare && !(all > 0.)) {
+    which = 1;
+    all = 0.;
+    for (int k = l; k < a.pieces; k += 64) all += held(k, 1);
+    all = lane_of(upto(all), 63);
+  }
+  const double goal = chance(lot[0]) * all;
+  found = false;
   double before = 0., sum = 0.;
   int place = 0;  // the first piece whose sum passes the goal, or the last that holds anything
   for (int k = 0; k < a.pieces; k += 64) {
-    const double z = held(k + l, which), up = upto(z);
+    const double z = amount(k + l), up = upto(z);
     const uint64_t past = __ballot(z > 0. && sum + up > goal), any = __ballot(z > 0.);
     if (any) {
       const int i = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(any);
@@ -603,7 +665,7 @@ __global__ void __launch_bounds__(kWalkers) verify_walk_kernel(VerifyArgs a) {
     if (past) break;
     sum += lane_of(up, 63);
   }
-  weigh(place);
+  weigh(place, bare && scale2 == 0.);
   if (which) {
 #pragma unroll
     for (int i = 0; i < kEach; ++i) now[i] = was[i];
