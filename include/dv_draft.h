@@ -57,7 +57,7 @@ typedef struct dv_verify_args {
   int32_t vocab;         /* tokens, at most 2^24 */
   int32_t rows;          /* that the arrays over drafts have: at least the sum of q_len */
   const void* logits;    /* device [rows][logits_row]: the target's, of what follows each draft */
-  int64_t logits_row;    /* elements from row to row, at least vocab */
+  int64_t logits_row;    /* elements from row to row, at least vocab, at most 2^33 */
   const float* drawn;    /* device [rows][drawn_row], or NULL: the distribution that the drafts
                             which follow this one were drawn from */
   int64_t drawn_row;

@@ -237,19 +237,21 @@ __device__ __forceinline__ uint64_t shfl64(uint64_t x, int from) {
   return (uint64_t)(uint32_t)__shfl((int)(x >> 32), from) << 32 |
          (uint32_t)__shfl((int)x, from);
 }
+// What drafts l and l + 64 follow.
 template <bool WIDE>
-__device__ __forceinline__ Tree tree_of(const int32_t* parent, int nq) {
+__device__ __forceinline__ int2 parents_of(const int32_t* parent, int nq) {
+  const int l = threadIdx.x & 63;
+  return make_int2(l < nq ? parent[l] : -2, WIDE && l + 64 < nq ? parent[l + 64] : -2);
+}
+template <bool WIDE>
+__device__ __forceinline__ Tree tree_of(int2 parents, int nq) {
   const int l = threadIdx.x & 63;
   Tree t;
-  int p = l < nq ? parent[l] : -2;
+  int p = parents.x, p2 = parents.y;
   if (p < -1 || p >= l) p = -2;
+  if (p2 < -1 || p2 >= l + 64) p2 = -2;
   t.a = Line{1ull << l, 0};
   t.b = Line{0, 1ull << l};
-  int p2 = -2;
-  if (WIDE && nq > 64) {
-    p2 = l + 64 < nq ? parent[l + 64] : -2;
-    if (p2 < -1 || p2 >= l + 64) p2 = -2;
-  }
   for (int k = 1; k < nq; k <<= 1) {
     const int at = max(p, 0) & 63;
     const uint64_t up = shfl64(t.a.lo, at);
@@ -451,8 +453,8 @@ __global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
   f32x4* columns = (f32x4*)(tables + (a.slopes ? 4 : 3) * a.chunk);
   int* odd = (int*)(columns + RT * 16);
   const int base = len - nq;  // the queries' first slot
-  Tree tree;
-  if constexpr (TREE) tree = tree_of<false>(a.parent + seq.tok, nq);
+  int2 parents = {0, 0};
+  if constexpr (TREE) parents = parents_of<false>(a.parent + seq.tok, nq);
   const int64_t slab = 2 * (int64_t)a.layer;
   const uint8_t* kb = q.codes + slab * q.s_slab + sb * q.s_b + h * q.s_h;
   const uint8_t* vb = kb + q.s_slab;
@@ -477,11 +479,6 @@ __global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
       pos[i] = q.position ? from_last(q.position[slots + t], last_at) : (float)t;
     bad |= hole;
   }
-  if constexpr (TREE) {
-    const int i = base + l - c0;
-    if (a.slopes && wave == 0 && l < nq && i >= 0 && i < cn)
-      pos[i] = (float)(root_at + tree.a.depth());
-  }
 
   // The queries, and what each column (row c of tile rt) may see.
   u32x4 qr[kInLds ? 1 : RT][KS];
@@ -500,22 +497,14 @@ __global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
       if constexpr (!kInLds) qr[rt][s] = x;
       if (kInLds && mine) ql[(rt * KS + s) * 64] = x;
     }
-    Line line{0, 0};
-    if constexpr (TREE) line = line_of<false>(tree, i);
-    if (mine && g == 0) {
+    if (!TREE && mine && g == 0) {
       const int limit = on ? len - nq + i : -1;
       float slope = 0.f, here = 0.f;
-      if (a.slopes && limit >= 0 && !(TREE && !line.there())) {
+      if (a.slopes && limit >= 0) {
         slope = a.slopes[head] * kLog2e;
-        here = TREE         ? (float)(root_at + line.depth())
-               : q.position ? from_last(q.position[slots + limit], last_at)
-                            : (float)limit;
+        here = q.position ? from_last(q.position[slots + limit], last_at) : (float)limit;
       }
-      if constexpr (TREE)
-        columns[r] = f32x4{__uint_as_float(on ? (uint32_t)line.lo : 0u), slope, here,
-                           __uint_as_float(on ? (uint32_t)(line.lo >> 32) : 0u)};
-      else
-        columns[r] = f32x4{__int_as_float(limit), slope, here, 0.f};
+      columns[r] = f32x4{__int_as_float(limit), slope, here, 0.f};
     }
   }
   // (LDS is all that the workgroup shares so far: loads may stay in flight)
@@ -523,8 +512,9 @@ __global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
   if (l == 0) odd[wave] = any_bad;
   lds_barrier();
   const bool holes = odd[0] | odd[1] | odd[2] | odd[3];
-  // slots up to this one are seen by every row
-  const int all_see = !TREE ? len - nq : tree.gone ? -1 : base - 1;
+  int all_see = len - nq;  // slots up to this one are seen by every row
+  // (parents are waited for here, before the codes are asked for)
+  if constexpr (TREE) asm volatile("" : "+v"(parents.x));
 
   // Copy n of a half: tokens n * 64 / CH ..., lane's token l / CH of them, piece
   // l % CH of its place.  Pieces past head_dim repeat the row's first one: they
@@ -728,6 +718,27 @@ __global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
     fetch(kb, k_to, t);
     fetch(vb, k_to + kHalf, t);
   }
+  if constexpr (TREE) {  // while the first codes are on their way
+    const Tree tree = tree_of<false>(parents, nq);
+    all_see = tree.gone ? -1 : base - 1;
+    const int i = base + l - c0;
+    if (a.slopes && wave == 0 && l < nq && i >= 0 && i < cn)
+      pos[i] = (float)(root_at + tree.a.depth());
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const int r = rt * 16 + c, i = r / a.G, head = h * a.G + (r - i * a.G);
+      const bool on = r < rows;
+      const Line line = line_of<false>(tree, i);
+      if (rt % 4 != wave || g != 0) continue;
+      float slope = 0.f, here = 0.f;
+      if (a.slopes && on && line.there()) {
+        slope = a.slopes[head] * kLog2e;
+        here = (float)(root_at + line.depth());
+      }
+      columns[r] = f32x4{__uint_as_float(on ? (uint32_t)line.lo : 0u), slope, here,
+                         __uint_as_float(on ? (uint32_t)(line.lo >> 32) : 0u)};
+    }
+  }
   // The scales follow the first codes: both are on their way at once.
   for (int i = tid; i < ((cn + kSplitStep - 1) & -kSplitStep); i += kThreads) {
     const int blk = ((const int*)ks)[i];
@@ -899,15 +910,11 @@ __global__ void __launch_bounds__(kThreads, tile_waves(DP))
   const bool on = r < rows;
   const int i0 = r / a.G, head = h * a.G + (r - i0 * a.G);
   const int base = len - nq;  // the queries' first slot
-  Tree tree;
+  int2 parents = {0, 0};
+  if constexpr (TREE) parents = parents_of<true>(a.parent + seq.tok, nq);
   Line line{0, 0};
-  if constexpr (TREE) {
-    tree = tree_of<true>(a.parent + seq.tok, nq);
-    line = line_of<true>(tree, on ? i0 : 0);
-    if (!on) line = Line{0, 0};
-  }
-  const int limit = !on || (TREE && !line.there()) ? -1 : base + i0;
-  const int all_see = !TREE ? base + scalar(r0 / a.G) : tree.gone ? -1 : base - 1;
+  const int limit = on ? base + i0 : -1;
+  int all_see = base + scalar(r0 / a.G);
   const int last = len - nq + scalar((min(rows, r0 + kTileRows) - 1) / a.G);  // last slot seen
   const int begin = split * a.chunk, end = min(min(begin + a.chunk, len), last + 1);
   const int N = end > begin ? (end - begin + kTile - 1) / kTile : 0;
@@ -936,16 +943,24 @@ __global__ void __launch_bounds__(kThreads, tile_waves(DP))
   float slope = 0.f, here = 0.f;
   const int last_at = last_position(q, a.slopes, slots, TREE ? base : len);
   float* const draft_at = (float*)(lds + L::kDrafts);
-  if constexpr (TREE) {
+  // Trees: this row's line and position, and with slopes all drafts' positions.
+  auto plant = [&] {
+    const Tree tree = tree_of<true>(parents, nq);
+    const Line x = line_of<true>(tree, on ? i0 : 0);
+    if (on) line = x;
+    all_see = tree.gone ? -1 : base - 1;
     const int root_at = q.position ? base > 0 : base;  // a draft's position: this and its depth
-    if (a.slopes && limit >= 0) {
+    if (a.slopes && limit >= 0 && line.there()) {
       slope = a.slopes[head] * kLog2e;
       here = (float)(root_at + line.depth());
     }
-    if (a.slopes && wave == 0) {  // (before the first barrier; read after it)
+    if (a.slopes && wave == 0) {
       draft_at[l] = (float)(root_at + tree.a.depth());
       draft_at[l + 64] = (float)(root_at + tree.b.depth());
     }
+  };
+  if (TREE && a.slopes) {  // (the first segment's table needs the positions)
+    plant();
     __syncthreads();
   } else if (a.slopes && limit >= 0) {
     slope = a.slopes[head] * kLog2e;
@@ -1081,7 +1096,9 @@ __global__ void __launch_bounds__(kThreads, tile_waves(DP))
                                      : from_last(q.position[slots + slot], last_at);
     __syncthreads();
     holes = any_hole(0);
+    if constexpr (TREE) asm volatile("" : "+v"(parents.x), "+v"(parents.y));
     for (int n = 0; n < kAhead; ++n) fetch(n, N - 1);
+    if (TREE && !a.slopes) plant();  // while the first codes are on their way
     wait_loads<0>();
 #pragma unroll
     for (int i = 0; i < UT; ++i) {

@@ -58,8 +58,8 @@ int verify(const int32_t* q_len, const float* temperature, const dv_verify_args*
         !aligned4(u->path) || !aligned4(u->next) || !aligned4(u->drawn) ||
         (reinterpret_cast<uintptr_t>(u->logits) & (size - 1)) || !aligned16(u->workspace))
       return DV_ERR_INVALID;
-    // strides, also of tables far larger than memory, stay inside 64 bits of bytes
-    const int64_t most = 1ll << 40;
+    // fewer than 2^27 rows (the workspace's limit): their bytes stay inside 64 bits
+    const int64_t most = 1ll << 33;
     if (u->logits_row < u->vocab || u->logits_row > most) return DV_ERR_INVALID;
     if (u->drawn && (u->drawn_row < u->vocab || u->drawn_row > most)) return DV_ERR_INVALID;
     if (u->workspace_bytes < p.bytes) return DV_ERR_SPACE;

@@ -124,7 +124,7 @@ def test_verify_refusals():
     assert verify(workspace=WORK + 8) == INVALID and verify(logits=LOGITS + 2, type=2) == INVALID
     assert verify(drawn=DRAWN + 2, drawn_row=100) == INVALID
     assert verify(logits_row=99) == INVALID and verify(drawn=DRAWN, drawn_row=99) == INVALID
-    assert verify(logits_row=(1 << 40) + 1) == INVALID
+    assert verify(logits_row=(1 << 33) + 1) == INVALID
     for t in ([1, 1, -0.5], [1, np.nan, 1], [np.inf, 1, 1]):
         assert verify(temperature=t) == INVALID, t
     # what is written overlaps what is read, or each other
