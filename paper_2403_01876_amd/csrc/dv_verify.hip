@@ -348,6 +348,7 @@ template <int TYPE>
 __global__ void __launch_bounds__(kWalkers) verify_walk_kernel(VerifyArgs a) {
   __shared__ double total[kMaxDrafts], share[kMaxDrafts], part[kWaves], parts[kWaves], sums[kMaxDrafts];
   __shared__ float tops[kWaves];
+  __shared__ uint64_t firsts[2];
   __shared__ float top[kMaxDrafts], from[kMaxDrafts], lot[kMaxDrafts];
   __shared__ int arg[kMaxDrafts], token[kMaxDrafts], judges[kMaxDrafts], ends[kWaves][2];
   __shared__ bool last;
@@ -418,25 +419,42 @@ __global__ void __launch_bounds__(kWalkers) verify_walk_kernel(VerifyArgs a) {
     if (a.drawn) d = some(a.drawn[(int64_t)(tok + up) * a.drawn_row + x]);
   }
   __syncthreads();
-  if (tid < nq) {
+  const double error = a.drawn || scale2 == 0. ? 0. : scale2 > 0x1p100 ? 1. : kSumError;
+  if (wave < 2) {
+    bool passes = false;  // as the first that is tried, beyond doubt
     if (up >= 0) {
       const Scale scale{scale2, top[up], arg[up]};
-      share[tid] = total[up] == 0. ? 0. : scale.of(y, x);
+      const double sum = total[up], w = sum == 0. ? 0. : scale.of(y, x);
+      passes = chance(chance_of) * (a.drawn ? (double)d : 1.) * sum < w - sum * error;
+      share[tid] = w;
     }
-    from[tid] = d;
-    lot[tid] = chance_of;
-    token[tid] = x;
+    if (tid < nq) {
+      from[tid] = d;
+      lot[tid] = chance_of;
+      token[tid] = x;
+    }
+    const uint64_t bits = __ballot(passes);
+    if (l == 0) firsts[wave] = bits;
   }
   __syncthreads();
 
-  const double error = a.drawn || scale2 == 0. ? 0. : scale2 > 0x1p100 ? 1. : kSumError;
   const bool teller = tid == 0 && at == 0;
   int here = 0, n = 1, turns = 0;
   uint64_t gone0 = 0, gone1 = 0;  // drafts whose shares have left the row
   bool pending = false;           // whether the last rejection's sum is not known yet
   if (teller) a.path[tok] = 0;
-  while (judges[here] && total[here] != 0.) {
+  const uint64_t pass0 = firsts[0], pass1 = firsts[1];
+  for (;;) {
     uint64_t try0 = __ballot(up0 == here), try1 = __ballot(up1 == here);
+    if (!(try0 | try1)) break;
+    const int next = try0 ? __builtin_ctzll(try0) : 64 + __builtin_ctzll(try1);
+    if ((next < 64 ? pass0 >> next : pass1 >> (next - 64)) & 1) {  // most often
+      here = next;
+      if (teller) a.path[tok + n] = here;
+      ++n;
+      continue;
+    }
+    if (total[here] == 0.) break;
     const void* row = row_of<TYPE>(a, tok + here);
     const float* q = a.drawn ? a.drawn + (int64_t)(tok + here) * a.drawn_row : nullptr;
     const Scale scale{scale2, top[here], arg[here]};
