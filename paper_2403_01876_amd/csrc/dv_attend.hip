@@ -393,6 +393,10 @@ __device__ __forceinline__ void add_weights(const AttendArgs& a, const Seq& seq,
 // TB/s; one of 131071, 273 MB (and 34 MB of scores written) 62 us, 4.9 TB/s.  A
 // wave lives for 54 % of the first and 72 % of the second; 59 % of the 56 us of 64
 // rows (143 MB), whose registers hold two workgroups a CU.
+// Trees (TREE): the same but for the last slots, which a row sees by its draft's line (the
+// column's first and last word) instead of up to a limit, and for the drafts' positions.  16
+// sequences of 64 to 2048 tokens, 14 heads, 5 to 24 drafts, bias and positions, 63 MB: 23
+// us, 2.7 TB/s, and 5 for the join; a wave lives for 53 % of it.
 // ---------------------------------------------------------------------------
 // 16 bytes a lane from memory to LDS: to lds + 16 * lane.
 template <bool NT>
@@ -851,6 +855,10 @@ __global__ void __launch_bounds__(kThreads, split_waves(DP, RT))
 // 0.385 ms, 0.69 PFLOP/s, 57 % of what a large matrix product reaches.  (When this
 // took 0.51 ms, 64 rows a wave instead of 32 took 0.69, results moved between
 // register files, and 64 tokens a tile 0.54, spilled.)
+// Trees (TREE) as above; a row's line stays in its lane's registers.  32 sequences of 128 to
+// 4096 tokens, 8 heads of 8: 40 to 64 drafts, 113 GFLOP, 187 us, 0.60 PFLOP/s; 8 to 16
+// drafts, 26 GFLOP that tiles of 128 rows pad, 70 us.  One of 131071 under 25 drafts, 107
+// GFLOP in tiles of 128 and 72 rows, 174 us, 0.62 PFLOP/s.
 // ---------------------------------------------------------------------------
 constexpr int kTile = 32, kSegment = 256, kPerSegment = kSegment / kTile, kAhead = 4;
 

@@ -15,6 +15,10 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 // a time, so that a wave reads 512 contiguous bytes and writes 1024.  Codes times
 // powers of two are exact in both types but for f16's smallest; beyond the type's
 // largest number is that.
+// Bound by HBM: 1 byte read and 2 written per element.  378 MB (8 prompts of 512 to 1024
+// tokens, 40 heads of 128, two layers) 63 us, 6.0 TB/s; a step's 1 to 6 tokens of 32
+// sequences, 20 layers of 8 heads, 12 MB of rows of 128 bytes, 5.4 us, of which 2 are the
+// launch.
 // ---------------------------------------------------------------------------
 template <bool BF16>
 __device__ __forceinline__ uint32_t two(uint32_t w, bool high, float scale, bool large) {
@@ -85,6 +89,9 @@ __global__ void __launch_bounds__(kThreads) quant_out_kernel(QuantArgs a) {
 // slots or later ones, so that a wave which has read a block's (or, of larger blocks,
 // 64 units of 16 codes of it, in order) may write over them.  Zeros under any scale stay
 // zeros: the ratio of scales is kept finite.
+// Bound by latency: four rounds through memory, of rows of 128 bytes that lie megabytes
+// apart.  32 sequences, 8 heads, 20 layers, 1 to 8 tokens each, 11 MB: 12 us; a wave for
+// each half took 13, and reading a block only once the last was written no less.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ float amax_of(const u32x4& c, float scale, float m) {
 #pragma unroll
