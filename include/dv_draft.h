@@ -88,7 +88,7 @@ DV_API int dv_verify_bytes(const int32_t* q_len, const dv_verify_args* a, uint64
  *              else r(x) becomes 0, and r is divided by its sum
  * (r stays as it is where that leaves nothing), and where it was accepted r = p(i).
  * At the end next is the lowest token y with r(0) + ... + r(y) above uniform[0].
- * Sums are held in 64 bits.  A logit that is NaN counts as -infinity; infinite ones
+ * All of it is decided as by sums in 64 bits.  A logit that is NaN counts as -infinity; infinite ones
  * share all probability.  A draft with a token outside [0, vocab), or that is not
  * there, is passed over.  drawn[i][x] counts as 0 where it is negative or NaN.  A row
  * whose logits are all -infinity accepts nothing; next is then -1.  A number outside

@@ -250,8 +250,8 @@ __global__ void __launch_bounds__(kThreads) verify_sums_kernel(VerifyArgs a) {
 #pragma unroll
         for (int k = 0; k < kPer<TYPE>; ++k)
           part += __builtin_amdgcn_exp2f(__builtin_fmaf(raw<TYPE>(w[i], k), s, c));
-      // Some NaN, or numbers that pass f32 on the way: each by itself.
-      if (__any(!(part < INFINITY)) || !(fabsf(c) < 0x1p100f)) {
+      // Some NaN, or numbers so large that c's rounding is of the size of t: each by itself.
+      if (__any(!(part < INFINITY)) || !(fabsf(c) < 0x1p20f)) {
         part = 0.f;
 #pragma unroll 1
         for (int u = first; u < start + kPiece; u += 64 * kPer<TYPE>)

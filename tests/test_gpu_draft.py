@@ -299,6 +299,23 @@ def test_verify_next_to_the_border(dtype):
         assert got[0].tolist()[:2] == [0, 5]
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("size", [1e4, 1e7, 1e10, 1e30, 3e38])
+def test_verify_logits_of_any_size(dtype, size):
+    """Offsets and spreads that 32 bits round: a few logits next to the largest share it."""
+    rng = np.random.default_rng(8)
+    for shift in (size, -size, 0.0):
+        x = torch.from_numpy(rng.normal(size=(6, 4500)) * size * 1e-3 + shift).clamp(-3.3e38, 3.3e38)
+        x = x.to(TYPES[dtype])
+        top = x.max(-1, keepdim=True).values
+        x[:, 7:4000:400] = top                         # ten equal ones
+        x[:, 9] = torch.nextafter(top[:, 0].float(), torch.tensor(-np.inf)).to(x.dtype)
+        token = rng.choice([7, 9, 407, 3], 6)
+        for T in (0.7, 1e-3, size * 1e-4):
+            run_verify([6], 4500, TYPES[dtype], rng, shape="star", logits=x, token=token,
+                       temperature=np.full(1, T, np.float32), border=1e-11)
+
+
 def test_verify_special_logits():
     """Infinities, NaN, rows without any probability; greedy and not."""
     rng = np.random.default_rng(1)
