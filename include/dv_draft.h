@@ -16,8 +16,8 @@
  * have a row for each, those of sequence b from row sum_{b' < b} q_len[b'] on.
  * parent[row of draft i] (device int32) is the draft that draft i follows, below i;
  * -1 where it follows the tokens before the drafts.  Any other value, on the way up
- * too, takes a draft out: it is not there.  A draft's line is itself and all that it
- * follows; its depth is how many those are.
+ * too, takes a draft out: it is not there.  A draft's line is itself and all drafts that
+ * it follows; its depth is how many it follows, 0 of draft 0.
  * A step: draft 0 is the last token that was sampled, not yet in the cache before,
  * and the others guess on from it.
  */
@@ -121,7 +121,8 @@ DV_API int dv_keep_path(const dv_quant* c, int32_t mb, int32_t l0, int32_t l1,
 
 /* dv_quant_in's way back: tokens [t0[b], t1[b]) of every sequence, layers [l0, l1), of
  * microbatch `mb` of `src` as the wire of these ranges with 2-byte elements of
- * `type` (t0 may be NULL: all zero), into `dst` of `dst_cap` bytes, 16-byte aligned.
+ * `type` (t0 may be NULL: all zero), into `dst` (device, 16-byte aligned) of `dst_cap`
+ * bytes.
  * Each element is its code times its scale, to the nearest (ties to even; exact but
  * for f16's multiples of 2^-24); beyond the type's largest number it is that, NaN is
  * NaN.  On return *out_bytes (if not NULL) holds the wire's size, also on

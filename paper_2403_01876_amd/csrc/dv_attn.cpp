@@ -189,8 +189,9 @@ void fill_tree(dv::AttendArgs* a, const int32_t* q_len, const int32_t* kv_len, i
     tok += q_len[b0 + i];
   }
   if (sorted)
-    std::stable_sort(order, order + nseq,
-                     [&](int32_t x, int32_t y) { return kv_len[b0 + x] > kv_len[b0 + y]; });
+    std::sort(order, order + nseq, [&](int32_t x, int32_t y) {  // equal ones in the batch's order
+      return kv_len[b0 + x] != kv_len[b0 + y] ? kv_len[b0 + x] > kv_len[b0 + y] : x < y;
+    });
   int64_t item = 0;
   for (int i = 0; i < kQSeqs; ++i) {
     const int64_t b = i < nseq ? b0 + order[i] : b0;
