@@ -172,6 +172,9 @@ __device__ __forceinline__ void larger(float& top, int& arg, float x, int i) {
 // 24.7 us a call, of 4096 26.3, of 8192 31.)
 // ---------------------------------------------------------------------------
 constexpr double kSumError = 0x1p-15;
+// A pass over the row in 64 bits: 512 threads add up 2^15 of 2^24 shares each, one after
+// another, which errs by 2^-38 of the sum; taking 127 of them away again, by 2^-46 of it.
+constexpr double kPassError = 0x1p-36;
 
 template <int TYPE, bool EXACT>
 __global__ void __launch_bounds__(kThreads) verify_sums_kernel(VerifyArgs a) {
@@ -272,7 +275,8 @@ __global__ void __launch_bounds__(kThreads) verify_sums_kernel(VerifyArgs a) {
 // are tried in order, of which a wave sees with one ballot those that follow the draft
 // accepted last.  With Z the sum of what is left of a row (its shares, relative to its
 // largest logit),
-//   not drawn: a rejected token's share leaves Z,
+//   not drawn: a rejected token's share leaves Z, which takes a pass over the row where the
+//          comparison lies within the error of Z or little is left,
 //   drawn: what is left of a token's share w becomes max(w - q Z, 0), whose sum takes a
 //          pass over the row where another draft is to be tried against it.
 // Then each workgroup adds up its pieces of what is left in 64 bits, and the one that
@@ -467,20 +471,26 @@ __global__ void __launch_bounds__(kWalkers) verify_walk_kernel(VerifyArgs a) {
     const void* row = row_of<TYPE>(a, tok + here);
     const float* q = a.drawn ? a.drawn + (int64_t)(tok + here) * a.drawn_row : nullptr;
     const Scale scale{scale2, top[here], arg[here]};
-    // The sum over the row's tokens of what is left of them.
-    auto pass = [&](int rejections) {
+    // The sum over the row's tokens of what is left of them, those of drafts out0 and out1 aside.
+    auto pass = [&](int rejections, uint64_t out0, uint64_t out1) {
       double sum = 0.;
       const int lead = lead_of<TYPE>(row);
 #pragma unroll 1
       for (int first = tid * 4 - lead; first < a.vocab; first += kWalkers * 4) {
-        const f32x4 z = four<TYPE>(row, first, a.vocab);
+        f32x4 z = four<TYPE>(row, first, a.vocab);
         f32x4 d = {0, 0, 0, 0};
         if (q) d = drawn_four(q, first, a.vocab);
+        for (uint64_t g = out0, h = out1; g | h;) {
+          const int y = token[next_of(g, h)] - first;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) z[i] = i == y ? -INFINITY : z[i];
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) sum += after(scale.of(z[i], first + i), d[i], total[here], sums, rejections);
       }
       return sum_all(sum, part);
     };
+    // Not drawn: `left` may be off by this much.
     double left = total[here], off = left * error;
     int taken = -1;
     while (try0 | try1) {
@@ -489,7 +499,7 @@ __global__ void __launch_bounds__(kWalkers) verify_walk_kernel(VerifyArgs a) {
       double r = share[i];
       if (q) {
         if (pending) {  // the sum of what the last rejection left
-          const double sum = pass(turns + 1);
+          const double sum = pass(turns + 1, 0, 0);
           if (sum > 0.) {
             ++turns;
             left = sum;
@@ -503,20 +513,22 @@ __global__ void __launch_bounds__(kWalkers) verify_walk_kernel(VerifyArgs a) {
         const int x = token[i];  // the second guess of a token has nothing left
         if ((__ballot(up0 == here && x0 == x) & gone0) | (__ballot(up1 == here && x1 == x) & gone1))
           r = 0.;
-        if (fabs(u * left - r) <= off || (u * left >= r && left - r <= off)) {
-          // Too near to tell, or nothing may be left: the row once more, in 64 bits.
-          const double sum = pass(0);
-          left += sum - total[here];
-          off = 0.;
-          __syncthreads();
-          if (tid == 0) total[here] = sum;
-          __syncthreads();
+        const uint64_t bit0 = i < 64 ? 1ull << i : 0, bit1 = i < 64 ? 0 : 1ull << (i & 63);
+        double rest = left - r;
+        if (r > 0. && (fabs(u * left - r) <= off || (u * left >= r && rest <= off))) {
+          // Too near to tell, or little may be left: what the other tokens hold, added up in 64
+          // bits.  A difference would err by the size of what it is taken from; this sum is 0
+          // where nothing is left, and else right to its own size.
+          rest = pass(0, gone0 | bit0, gone1 | bit1);
+          left = rest + r;
+          off = rest * kPassError;
         }
         if (u * left < r) {
           taken = i;
-        } else if (r > 0. && left - r > 0.) {
-          left -= r;
-          (i < 64 ? gone0 : gone1) |= 1ull << (i & 63);
+        } else if (r > 0. && rest > 0.) {
+          left = rest;
+          gone0 |= bit0;
+          gone1 |= bit1;
         }
       }
       if (taken >= 0) break;

@@ -1,0 +1,140 @@
+"""Verification where rounding could decide: guesses that cover all that has any
+probability, remainders far below the rounding of what they are left from, numbers at and
+past the end of [0, 1).
+
+Results are whole numbers and have to be equal to the plain 64-bit form's.  A number of 1 or
+more lets no draft pass whatever the rounding, so such draws need no distance from a border;
+draws with others are made anew until their closest decision lies 1e-9 from its border, and
+a test without a clear draw fails.
+"""
+import numpy as np
+import pytest
+import torch
+
+from tests import draft_ref as dref
+from tests.test_gpu_draft import TYPES, run_verify
+
+pytestmark = pytest.mark.gpu
+
+
+def run_clear(draws, border=1e-9):
+    """run_verify of the first of `draws` (dictionaries of its arguments) that is clear of
+    its borders."""
+    for kw in draws:
+        try:
+            return run_verify(**kw, border=border)
+        except pytest.skip.Exception:
+            pass
+    raise AssertionError("no draw was clear of its borders")
+
+
+def masked(B, most, V, live, rng, spread=2.0):
+    """Logits of B sequences of `most` drafts, all but `live` tokens of each row -infinity, and
+    those tokens [B, live]: some next to each other on both sides of 2048."""
+    x = torch.full((B * most, V), -np.inf)
+    tokens = np.empty((B, live), np.int64)
+    for b in range(B):
+        near = 2048 - live // 2 + np.arange(live)
+        at = near if b % 3 == 0 and V > 2048 + live else rng.choice(V, live, replace=False)
+        tokens[b] = rng.permutation(at)
+        for row in range(b * most, (b + 1) * most):
+            x[row, at] = torch.from_numpy(rng.normal(size=live) * spread).float()
+    return x, tokens
+
+
+def stars(tokens, rng, again):
+    """Drafts that guess all of `tokens` after the first row, `again` of them twice: how
+    many drafts a sequence has, and all their tokens."""
+    guesses = [np.concatenate([[0], rng.permutation(np.concatenate([t, t[:again]]))]) for t in tokens]
+    return len(guesses[0]), np.concatenate(guesses)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("live", [2, 3, 4, 5, 40])
+@pytest.mark.parametrize("again", [0, 2])
+def test_guesses_of_all_that_is_left(dtype, live, again):
+    """Every token with any probability is guessed and refused: the last of them stays, and
+    is what follows."""
+    rng = np.random.default_rng(live + 100 * again)
+    B, V = 64, 4500
+    for u in (1.0, np.nan, 2.0):
+        x, tokens = masked(B, 1 + live + again, V, live, rng)
+        most, token = stars(tokens, rng, again)
+        uniform = np.full(B * most, u, np.float32)
+        uniform[::most] = rng.choice([0.0, 0.25, 0.5, 0.999, 1.0], B)
+        got = run_verify([most] * B, V, TYPES[dtype], rng, shape="star", logits=x.to(TYPES[dtype]),
+                         token=token, uniform=uniform, border=0.0,
+                         temperature=rng.uniform(0.5, 2, B).astype(np.float32))
+        assert (got[1] == 1).all()
+        last = [list(dict.fromkeys(g))[-1] for g in token.reshape(B, most)[:, 1:].tolist()]
+        assert got[2].tolist() == last
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_guesses_of_all_that_is_left_among_others(seed):
+    """The same with ordinary numbers among those past the end."""
+    rng = np.random.default_rng(seed)
+    B, V, live = 48, 3001, 3 + seed
+
+    def draws():
+        for _ in range(20):
+            x, tokens = masked(B, 1 + live, V, live, rng)
+            most, token = stars(tokens, rng, 0)
+            u = np.where(rng.random(B * most) < 0.4, rng.random(B * most), 1.0)
+            yield dict(q_len=[most] * B, V=V, dtype=torch.float32, rng=rng, shape="star", logits=x,
+                       token=token, uniform=u)
+    run_clear(draws())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_remainder_far_below_the_rest(dtype):
+    """What is left of a row may be 1e-20 or 1e-200 of it: it is what counts from there on."""
+    rng = np.random.default_rng(4)
+    B, V = 32, 2500
+    for gap in (45.0, 60.0, 200.0):
+        x = torch.full((B * 4, V), -np.inf)
+        token = np.zeros((B, 4), np.int64)
+        for b in range(B):
+            at = rng.choice(V, 5, replace=False)
+            x[b * 4:b * 4 + 4, at] = torch.tensor([0.0, -gap, -gap - 1, -gap - 0.5, -2 * gap])
+            token[b, 1:] = at[[0, 1, 3] if b % 2 else [0, 4, 2]]
+        uniform = np.full(B * 4, 1.0, np.float32)
+        uniform[::4] = rng.choice([0.0, 0.125, 0.5, 0.875], B)
+        got = run_verify([4] * B, V, TYPES[dtype], rng, shape="star", logits=x.to(TYPES[dtype]),
+                         token=token.reshape(-1), uniform=uniform, border=0.0)
+        assert (got[1] == 1).all()
+
+
+@pytest.mark.parametrize("side", [-1, 1])
+def test_rejections_of_nearly_all_there_is(side):
+    """Two rejections leave 2^-44 of a row; the third guess is decided 1e-5 from its border,
+    which sums that err by 2^-53 of the whole row would not tell."""
+    rng = np.random.default_rng(9)
+    V, e = 3000, 2.0 ** -22
+    x = torch.full((4 * 16, V), -np.inf)
+    token, uniform = [], []
+    for b in range(16):
+        at = rng.choice(V, 4, replace=False)
+        share = rng.uniform(0.3, 0.7)
+        # shares e^... of the row: nearly all, nearly all of the rest, and two of what is left
+        x[4 * b, at] = torch.tensor([0.0, np.log(e), 2 * np.log(e) + np.log(share),
+                                     2 * np.log(e) + np.log(1 - share)]).float()
+        p = dref.target(x[4 * b].double().numpy(), 1.0)
+        u3 = p[at[2]] / (p[at[2]] + p[at[3]]) * (1 + side * 1e-5)
+        token += [0, *at[:3]]
+        uniform += [rng.random(), 1 - 2.0 ** -24, 1 - 2.0 ** -24, u3]
+    got = run_verify([4] * 16, V, torch.float32, rng, shape="star", logits=x, token=token,
+                     uniform=uniform, border=1e-8)
+    assert (got[1] == (1 if side > 0 else 2)).all()
+
+
+def test_many_guesses_of_all_that_is_left():
+    """127 guesses that cover a row, on both sides of several pieces."""
+    rng = np.random.default_rng(6)
+    B, V = 4, 9001
+    x, tokens = masked(B, 128, V, 127, rng, 1.0)
+    most, token = stars(tokens, rng, 0)
+    uniform = np.full(B * most, 1.0, np.float32)
+    got = run_verify([most] * B, V, torch.float32, rng, shape="star", logits=x, token=token,
+                     uniform=uniform, border=0.0)
+    assert got[2].tolist() == token.reshape(B, most)[:, -1].tolist()
