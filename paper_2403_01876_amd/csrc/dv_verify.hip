@@ -689,7 +689,8 @@ __global__ void __launch_bounds__(kWalkers) verify_walk_kernel(VerifyArgs a) {
     for (int k = l; k < a.pieces; k += 64) all += held(k, 1);
     all = lane_of(upto(all), 63);
   }
-  const double goal = chance(lot[0]) * all;
+  // (1 passes no sum: as a product it could, where sums of other groupings round up)
+  const double u = chance(lot[0]), goal = u < 1. ? u * all : INFINITY;
   found = false;
   double before = 0., sum = 0.;
   int place = 0;  // the first piece whose sum passes the goal, or the last that holds anything

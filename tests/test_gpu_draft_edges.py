@@ -138,3 +138,21 @@ def test_many_guesses_of_all_that_is_left():
     got = run_verify([most] * B, V, torch.float32, rng, shape="star", logits=x, token=token,
                      uniform=uniform, border=0.0)
     assert got[2].tolist() == token.reshape(B, most)[:, -1].tolist()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("drawn", [False, True])
+@pytest.mark.parametrize("V,B", [(900, 64), (5000, 64), (140001, 12)])
+def test_a_number_of_one_takes_the_last_token(V, B, drawn, dtype):
+    """However little the last token holds beside the rest: shares down to 1e-150."""
+    rng = np.random.default_rng(V)
+    n = rng.integers(1, 4, B)
+    for u0 in (1.0, 2.0, np.nan):
+        def draws():
+            for _ in range(20):
+                u = rng.random(n.sum())
+                u[np.cumsum(n) - n] = u0
+                yield dict(q_len=n, V=V, dtype=TYPES[dtype], rng=rng, drawn=drawn, uniform=u,
+                           temperature=rng.uniform(0.06, 0.3, B).astype(np.float32),
+                           logits=torch.from_numpy(rng.normal(size=(n.sum(), V)) * 2).to(TYPES[dtype]))
+        run_clear(draws())
