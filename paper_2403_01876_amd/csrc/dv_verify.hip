@@ -259,7 +259,8 @@ __global__ void __launch_bounds__(kThreads) verify_sums_kernel(VerifyArgs a) {
 #pragma unroll 1
         for (int u = first; u < start + kPiece; u += 64 * kPer<TYPE>)
           for (int k = max(u, 0); k < min(u + kPer<TYPE>, a.vocab); ++k)
-            part += __builtin_amdgcn_exp2f((one_of<TYPE>(p, k) - top) * s);
+            // (halves: the difference of two logits may lie beyond 32 bits' range)
+            part += __builtin_amdgcn_exp2f((0.5f * one_of<TYPE>(p, k) - 0.5f * top) * (2.f * s));
       } else {
         part *= __builtin_amdgcn_exp2f(__builtin_fmaf(-top, s, -c));
       }

@@ -1,6 +1,6 @@
 """Verification where rounding could decide: guesses that cover all that has any
 probability, remainders far below the rounding of what they are left from, numbers at and
-past the end of [0, 1).
+past the end of [0, 1), logits whose differences 32 bits do not hold.
 
 Results are whole numbers and have to be equal to the plain 64-bit form's.  A number of 1 or
 more lets no draft pass whatever the rounding, so such draws need no distance from a border;
@@ -156,3 +156,23 @@ def test_a_number_of_one_takes_the_last_token(V, B, drawn, dtype):
                            temperature=rng.uniform(0.06, 0.3, B).astype(np.float32),
                            logits=torch.from_numpy(rng.normal(size=(n.sum(), V)) * 2).to(TYPES[dtype]))
         run_clear(draws())
+
+
+def test_logits_as_far_apart_as_they_come():
+    """Differences of logits past 32 bits' range, under temperatures that make them count, in
+    rows with NaN and without."""
+    rng = np.random.default_rng(3)
+    B, V = 32, 300
+    x = torch.full((2 * B, V), -np.inf)
+    token, uniform = [], []
+    for b in range(B):
+        at = rng.choice(V, 4, replace=False)
+        x[2 * b, at] = torch.tensor([3.3e38, -3.3e38, -3.2e38, -3.1e38])
+        if b % 2:
+            x[2 * b, rng.choice(np.setdiff1d(np.arange(V), at))] = np.nan
+        p = dref.target(x[2 * b].double().numpy(), 3e38)
+        token += [0, at[b // 2 % 2]]
+        uniform += [rng.random(), p[token[-1]] * (1.02 if b % 4 < 2 else 0.98)]
+    got = run_verify([2] * B, V, torch.float32, rng, shape="chain", logits=x, token=token,
+                     uniform=uniform, temperature=np.full(B, 3e38, np.float32))
+    assert got[1].tolist() == [1 if b % 4 < 2 else 2 for b in range(B)]
