@@ -4,7 +4,8 @@
 ``dv_attend_tree`` runs one layer's attention of drafted tokens that branch,
 ``dv_verify`` accepts drafts by the target model's logits and given random numbers,
 ``dv_keep_path`` moves the accepted ones together in the cache, and ``dv_quant_out``
-reads cached tokens back as a 16-bit stream.
+reads cached tokens back as a 16-bit stream.  Tensors have to be on one GPU, or in pinned
+memory of the host: others are refused.
 """
 from __future__ import annotations
 
@@ -56,6 +57,21 @@ def _array(name: str, x, dtype, least: int = 0):
     return x.data_ptr()
 
 
+def _astray(**tensors) -> str:
+    """For a refusal's name, which tensors a GPU would not reach: those in the host's pageable
+    memory, or on another GPU than the first that is on one.  Empty if there are none."""
+    device, names = -1, []
+    for name, x in tensors.items():
+        if x is None or x.numel() == 0:
+            continue
+        at = x.get_device()
+        if at < 0 and not x.is_pinned() or at >= 0 and device not in (-1, at):
+            names.append(name)
+        elif device < 0:
+            device = at
+    return f" ({', '.join(names)}: not in the GPU's memory)" if names else ""
+
+
 def _lengths(name: str, x):
     """One-dimensional int32 lengths: the array, its address and size."""
     n = len(x)
@@ -84,8 +100,17 @@ def dv_attend_tree(c: QuantCache, mb: int, layer: int, q_len, kv_len, parent, q,
     a = _attend_args(c, q, out, scale, slopes, None, lse, workspace)
     at = _array("parent", parent, torch.int32)
     a.rows = min(a.rows, parent.numel())
+    name, d = "dv_attend_tree", q.get_device()
+    # (the usual case asked for at once: a call is bound by the host where texts are short)
+    if d < 0 or out.get_device() != d or parent.get_device() != d or \
+            (slopes is not None and slopes.get_device() != d) or \
+            (lse is not None and lse.get_device() != d) or \
+            (workspace is not None and workspace.get_device() != d):
+        name += _astray(q=q, out=out, parent=parent, slopes=slopes, lse=lse, workspace=workspace)
+        if name != "dv_attend_tree":  # refused, after what else there is to refuse
+            at = None
     rc = lib.dv_attend_tree(c.ref, mb, layer, p0, p1, at, ctypes.byref(a), _stream(stream))
-    return _check(rc, "dv_attend_tree", check)
+    return _check(rc, name, check)
 
 
 def _table(name: str, x, types):
@@ -142,8 +167,12 @@ def dv_verify(q_len, parent, token, logits, uniform, path, count, next, temperat
                        _array("uniform", uniform, torch.float32), _array("path", path, i32),
                        _array("count", count, i32, batch), _array("next", next, i32, batch),
                        _addr(workspace), wb)
+    astray = _astray(logits=logits, drawn=drawn, parent=parent, token=token,
+                     uniform=uniform, path=path, count=count, next=next, workspace=workspace)
+    if astray:
+        a.count = None
     rc = lib.dv_verify(p, ta, ctypes.byref(a), _stream(stream))
-    return _check(rc, "dv_verify", check)
+    return _check(rc, "dv_verify" + astray, check)
 
 
 def dv_keep_path(c: QuantCache, mb: int, l0: int, l1: int, q_len, kv_len, path, count,
@@ -153,10 +182,15 @@ def dv_keep_path(c: QuantCache, mb: int, l0: int, l1: int, q_len, kv_len, path, 
     batch = c.cache.c.batch
     a0, p0 = _i32(q_len, batch)
     a1, p1 = _i32(kv_len, batch)
-    path = _array("path", path, torch.int32, 0 if a0 is None else sum(a0.tolist()))
-    count = _array("count", count, torch.int32, batch)
-    rc = lib.dv_keep_path(c.ref, mb, l0, l1, p0, p1, path, count, _stream(stream))
-    return _check(rc, "dv_keep_path", check)
+    at = _array("path", path, torch.int32, 0 if a0 is None else sum(a0.tolist()))
+    n = _array("count", count, torch.int32, batch)
+    name = "dv_keep_path"
+    if path.get_device() < 0 or path.get_device() != count.get_device():
+        name += _astray(path=path, count=count)
+        if name != "dv_keep_path":
+            at = None
+    rc = lib.dv_keep_path(c.ref, mb, l0, l1, p0, p1, at, n, _stream(stream))
+    return _check(rc, name, check)
 
 
 def dv_quant_out(src: QuantCache, mb: int, l0: int, l1: int, t0, t1, dst, dst_cap: int,
@@ -165,8 +199,12 @@ def dv_quant_out(src: QuantCache, mb: int, l0: int, l1: int, t0, t1, dst, dst_ca
     bytes (with check=False: status and bytes)."""
     a0, p0 = _i32(t0, src.cache.c.batch)
     a1, p1 = _i32(t1, src.cache.c.batch)
-    out = _u64(0)
-    rc = lib.dv_quant_out(src.ref, mb, l0, l1, p0, p1, _addr(dst), dst_cap, type,
-                          ctypes.byref(out), _stream(stream))
-    _check(rc, "dv_quant_out", check)
+    out, at, name = _u64(0), _addr(dst), "dv_quant_out"
+    if isinstance(dst, np.ndarray) or isinstance(dst, torch.Tensor) and dst.get_device() < 0:
+        name += _astray(dst=torch.as_tensor(dst))
+        if name != "dv_quant_out":
+            at = None
+    rc = lib.dv_quant_out(src.ref, mb, l0, l1, p0, p1, at, dst_cap, type, ctypes.byref(out),
+                          _stream(stream))
+    _check(rc, name, check)
     return out.value if check else (rc, out.value)

@@ -1,6 +1,7 @@
 """Verification where rounding could decide: guesses that cover all that has any
 probability, remainders far below the rounding of what they are left from, numbers at and
-past the end of [0, 1), logits whose differences 32 bits do not hold.
+past the end of [0, 1), logits whose differences 32 bits do not hold; and where results
+may lie.
 
 Results are whole numbers and have to be equal to the plain 64-bit form's.  A number of 1 or
 more lets no draft pass whatever the rounding, so such draws need no distance from a border;
@@ -11,8 +12,9 @@ import numpy as np
 import pytest
 import torch
 
+from paper_2403_01876_amd import draft, dv
 from tests import draft_ref as dref
-from tests.test_gpu_draft import TYPES, run_verify
+from tests.test_gpu_draft import TYPES, logits_of, run_verify
 
 pytestmark = pytest.mark.gpu
 
@@ -176,3 +178,26 @@ def test_logits_as_far_apart_as_they_come():
     got = run_verify([2] * B, V, torch.float32, rng, shape="chain", logits=x, token=token,
                      uniform=uniform, temperature=np.full(B, 3e38, np.float32))
     assert got[1].tolist() == [1 if b % 4 < 2 else 2 for b in range(B)]
+
+
+def test_results_in_pinned_memory_and_none_in_pageable():
+    """What a step reads on the host may lie in pinned memory; pageable memory is refused."""
+    q_len, V = [5, 0, 9], 3000
+    rows = sum(q_len)
+    rng = np.random.default_rng(1)
+    ints = torch.from_numpy(dref.trees(q_len, rng)).cuda()
+    token = torch.from_numpy(rng.integers(0, V, rows).astype(np.int32)).cuda()
+    x, u = logits_of(rows, V, rng, torch.float32).cuda(), torch.rand(rows, device="cuda")
+    room = torch.empty(draft.dv_verify_bytes(q_len, x), dtype=torch.uint8, device="cuda")
+
+    def results(**where):
+        return [torch.full((n,), -7, dtype=torch.int32, **where) for n in (rows, 3, 3)]
+    a, b, host = results(device="cuda"), results(pin_memory=True), results()
+    for r in (a, b):
+        draft.dv_verify(q_len, ints, token, x, u, *r, workspace=room)
+    torch.cuda.synchronize()
+    assert all(torch.equal(y.cpu(), z) for y, z in zip(a, b))
+    with pytest.raises(dv.DvError, match=r"\(path, count, next: not in"):
+        draft.dv_verify(q_len, ints, token, x, u, *host, workspace=room)
+    torch.cuda.synchronize()
+    assert all((h == -7).all() for h in host)
