@@ -1,4 +1,8 @@
-"""Refusals of the operators over drafted tokens, without a GPU: tensors that no GPU reaches."""
+"""Refusals and sizes of the operators over drafted tokens, without a GPU: tensors that no GPU
+reaches, and workspaces as large as a verification's pieces."""
+import ctypes
+
+import numpy as np
 import pytest
 import torch
 
@@ -118,3 +122,16 @@ def test_keep_and_out_refuse_tensors_that_no_gpu_reaches(launched):
     assert not any(whole for name, whole in launched if name == "dv_quant_out")
     draft.dv_quant_out(qc, 0, 0, 1, [0], [4], there(wire, SRC), wire.numel() * 2, attn.DV_F16)
     assert launched[-1] == ("dv_quant_out", True)
+
+
+@pytest.mark.parametrize("V,pieces", [(1, 1), (2041, 1), (2042, 2), (2048, 2), (2049, 2), (4089, 2),
+                                      (4090, 3), (32000, 16), (131071, 65), (1 << 24, 8193)])
+def test_verify_workspace_of_every_piece(V, pieces):
+    """Pieces of 2048 tokens, counted from up to seven tokens before a row's first: 16 bytes
+    for each piece of a row and of a sequence, and 4 for a sequence."""
+    for batch, q_len in ((1, [1]), (3, [5, 0, 128]), (65, [7] * 65)):
+        x = np.array(q_len, np.int32)
+        a = draft.dv_verify_args(type=attn.DV_BF16, batch=batch, vocab=V)
+        size = ctypes.c_uint64(0)
+        assert dv.lib.dv_verify_bytes(x.ctypes.data, ctypes.byref(a), ctypes.byref(size)) == 0
+        assert size.value == (sum(q_len) + batch) * pieces * 16 + batch * 4

@@ -1,7 +1,7 @@
 """Verification where rounding could decide: guesses that cover all that has any
 probability, remainders far below the rounding of what they are left from, numbers at and
-past the end of [0, 1), logits whose differences 32 bits do not hold; and where results
-may lie.
+past the end of [0, 1), logits whose differences 32 bits do not hold;
+vocabularies that end next to a piece; and where results may lie.
 
 Results are whole numbers and have to be equal to the plain 64-bit form's.  A number of 1 or
 more lets no draft pass whatever the rounding, so such draws need no distance from a border;
@@ -201,3 +201,35 @@ def test_results_in_pinned_memory_and_none_in_pageable():
         draft.dv_verify(q_len, ints, token, x, u, *host, workspace=room)
     torch.cuda.synchronize()
     assert all((h == -7).all() for h in host)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("drawn", [False, True])
+@pytest.mark.parametrize("V", [2040, 2041, 2042, 2047, 2048, 2049, 4088, 4089, 4090, 6143, 6145])
+def test_sizes_next_to_a_piece(dtype, drawn, V):
+    """Vocabularies that end next to a piece of 2048 tokens, in rows of an odd stride, which
+    begin at every place of 16 bytes."""
+    rng = np.random.default_rng(V)
+    q_len = [9, 1, 0, 11, 2]
+
+    def draws(shape):
+        for _ in range(20):
+            yield dict(q_len=q_len, V=V, dtype=TYPES[dtype], rng=rng, shape=shape, drawn=drawn,
+                       pad=1 - V % 2 + 2 * (V % 3),
+                       temperature=np.array([0.7, 1.3, 1.0, 0.0, 40.0], np.float32))
+    for shape in ("tree", "chain", "star"):
+        run_clear(draws(shape))
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_the_last_token_next_to_a_piece(dtype):
+    """One token has nearly all, the last of the vocabulary or the first of a piece: it is
+    accepted and follows, from every place that a row may begin at."""
+    for V in (2041, 2042, 2048, 2049, 4097):
+        for at in sorted({0, V - 1, min(2047, V - 1), min(2048, V - 1), V - 8}):
+            x = torch.zeros((16, V))
+            x[:, at] = 30.0
+            got = run_verify([16], V, TYPES[dtype], np.random.default_rng(at), shape="chain",
+                             logits=x.to(TYPES[dtype]), token=[at] * 16, pad=1 - V % 2,
+                             uniform=[0.5] * 16)
+            assert got[1].tolist() == [16] and got[2].tolist() == [at]
