@@ -85,11 +85,14 @@ template <int TYPE>
 __device__ __forceinline__ int lead_of(const void* row) {
   return (int)((uintptr_t)row & 15) / (TYPE == 2 ? 4 : 2);
 }
-// The logits of 16 bytes; nth: NaN as -infinity.
+// The logits of 16 bytes; nth: NaN as -infinity.  (Quieted: the larger of a signalling NaN and
+// a number is NaN where the compiler makes one maximum of three out of two.)
 template <int TYPE>
 __device__ __forceinline__ float raw(const u32x4& w, int i) {
-  if constexpr (TYPE == 2) return __uint_as_float(w[i]);
-  if constexpr (TYPE == 1) return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+  if constexpr (TYPE == 2) return __builtin_canonicalizef(__uint_as_float(w[i]));
+  if constexpr (TYPE == 1)
+    return __builtin_canonicalizef(
+        __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16));
   return (float)__builtin_bit_cast(_Float16, (uint16_t)(i & 1 ? w[i / 2] >> 16 : w[i / 2]));
 }
 template <int TYPE>

@@ -1,7 +1,7 @@
 """Verification where rounding could decide: guesses that cover all that has any
 probability, remainders far below the rounding of what they are left from, numbers at and
-past the end of [0, 1), logits whose differences 32 bits do not hold;
-vocabularies that end next to a piece; and where results may lie.
+past the end of [0, 1), logits whose differences 32 bits do not hold, NaN of every
+kind; vocabularies that end next to a piece; and where results may lie.
 
 Results are whole numbers and have to be equal to the plain 64-bit form's.  A number of 1 or
 more lets no draft pass whatever the rounding, so such draws need no distance from a border;
@@ -233,3 +233,30 @@ def test_the_last_token_next_to_a_piece(dtype):
                              logits=x.to(TYPES[dtype]), token=[at] * 16, pad=1 - V % 2,
                              uniform=[0.5] * 16)
             assert got[1].tolist() == [16] and got[2].tolist() == [at]
+
+
+@pytest.mark.parametrize("dtype,nans", [("f16", [0x7c01, 0x7e00, 0xfc01, 0xffff]),
+                                        ("bf16", [0x7f81, 0x7fc0, 0xff81, 0xffff]),
+                                        ("f32", [0x7f800001, 0x7fc00000, 0xff800001, 0xffffffff])])
+@pytest.mark.parametrize("drawn", [False, True])
+def test_nan_of_every_kind(dtype, nans, drawn):
+    """NaN, quiet and signalling, of either sign: none is a largest logit or part of a sum; with
+    an infinite logit and without."""
+    rng = np.random.default_rng(len(nans))
+    V, n = 4500, 8
+    bits = np.array(nans, np.uint32 if dtype == "f32" else np.uint16)
+    for infinite in (False, True):
+        def draws():
+            for _ in range(20):
+                x = logits_of(n, V, rng, TYPES[dtype])
+                y = x.numpy().view(bits.dtype) if dtype != "bf16" else \
+                    x.view(torch.int16).numpy().view(np.uint16)
+                for row in range(n):
+                    at = rng.choice(V, 200, replace=False)
+                    y[row, at] = rng.choice(bits, 200)
+                    if infinite and row % 2:
+                        x[row, rng.choice(V, 3, replace=False)] = np.inf
+                yield dict(q_len=[n], V=V, dtype=TYPES[dtype], rng=rng, drawn=drawn, logits=x,
+                           temperature=np.array([rng.choice([0.0, 0.8])], np.float32))
+        for _ in range(4):
+            run_clear(draws())
