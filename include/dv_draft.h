@@ -85,14 +85,20 @@ DV_API int dv_verify_bytes(const int32_t* q_len, const dv_verify_args* a, uint64
  *   drawn:     accept it where uniform[i] * drawn[a][x] < r(x);
  *              else r becomes max(r - drawn[a], 0) over its sum
  *   not drawn: accept it where uniform[i] < r(x);
- *              else r(x) becomes 0, and r is divided by its sum
+ *              else r(x) becomes 0, and r is divided by its sum, however little that is
  * (r stays as it is where that leaves nothing), and where it was accepted r = p(i).
  * At the end next is the lowest token y with r(0) + ... + r(y) above uniform[0].
- * All of it is decided as by sums in 64 bits.  A logit that is NaN counts as -infinity; infinite ones
- * share all probability.  A draft with a token outside [0, vocab), or that is not
- * there, is passed over.  drawn[i][x] counts as 0 where it is negative or NaN.  A row
- * whose logits are all -infinity accepts nothing; next is then -1.  A number outside
- * [0, 1) counts as the nearest end (1: the last token that r holds), NaN as 1.
+ * Drafts that follow one draft have to be drawn from drawn[a] independently, the same
+ * token twice if it comes so: of siblings drawn without replacement what is accepted is
+ * not distributed as the target's samples.  Drafts that were not drawn may be any tokens
+ * that do not depend on `uniform`.  A sibling that is tried after a drawn one was refused
+ * takes a pass over the row, the longer the more were refused.
+ * All of it is decided as by sums in 64 bits.  A logit that is NaN counts as -infinity;
+ * infinite ones share all probability.  Draft 0 is there whatever its parent; any other
+ * with a token outside [0, vocab), or that is not there, is passed over.  drawn[i][x]
+ * counts as 0 where it is negative or NaN.  A row whose logits are all -infinity accepts
+ * nothing; next is then -1.  A number outside [0, 1) counts as the nearest end (1: the
+ * last token that r holds), NaN as 1.
  * A sequence without drafts gets count 0 and its next is left as it is.
  * temperature: host [batch], finite, 0 or more; NULL: all 1.  What the call writes
  * must not overlap what it reads nor each other.
@@ -106,9 +112,10 @@ DV_API int dv_verify(const int32_t* q_len, const float* temperature, const dv_ve
  * and move them to slots base, base + 1, ... of microbatch `mb` of `c`, layers
  * [l0, l1): what dv_quant_in does with the numbers that they stand for, in place.
  * Blocks that hold tokens from before base keep the larger of their scale and the
- * kept ones' need, others get what their kept tokens need.  path: device int32
- * [rows], count: device int32 [batch].  A path ends before its first entry that is
- * not above the one before it, not below q_len[b] or negative, or after count[b].
+ * kept ones' need (also where only the append of rejected drafts had raised it), others
+ * get what their kept tokens need.  path: device int32 [rows], count: device int32
+ * [batch].  A path ends before its first entry that is not above the one before it, not
+ * below q_len[b] or negative, or after count[b].
  * Weights move along; positions stay, since a slot's is that of the token which
  * dv_quant_in would append there.  Slots past the kept ones hold nothing.  Tokens
  * of an unmapped block count as zeros; blocks that are not mapped are skipped.

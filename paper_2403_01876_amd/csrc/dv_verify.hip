@@ -290,7 +290,9 @@ __global__ void __launch_bounds__(kThreads) verify_sums_kernel(VerifyArgs a) {
 // Bound by latency, a dozen steps that wait for each other: 32 sequences of 4 to 9 drafts
 // over 32000 tokens 14 us, of 40 to 64 16, one sequence over 131071 13.  (512 threads: chains
 // 26.9 us a call, 256 27.8, 1024 28.4; sums by exchanges through LDS instead of moves
-// between lanes cost 4 us more.)
+// between lanes cost 4 us more.)  Passes are bound by exponentials, the whole row in every
+// workgroup: a call for 32 sequences of 2, 4 and 16 drawn siblings over 32000 tokens takes 38,
+// 82 and 565 us, since each pass goes through all rejections before it.
 // ---------------------------------------------------------------------------
 constexpr int kWalkers = 512, kWaves = kWalkers / 64;
 constexpr int kEach = kPiece / kWalkers;  // tokens of a piece that a thread takes, in order

@@ -139,7 +139,7 @@ def dv_verify(q_len, parent, token, logits, uniform, path, count, next, temperat
     """Accept drafts of every sequence by the target's ``logits`` [drafts, vocab] (float16,
     bfloat16 or float32): ``parent``, ``token`` (int32) and ``uniform`` (float32) hold a number
     for each draft, ``drawn`` (float32 [drafts, vocab], or None) the distributions that those
-    which follow them were drawn from.  ``path`` (int32 [drafts]), ``count`` and ``next`` (int32
+    which follow them were drawn from, independently of each other.  ``path`` (int32 [drafts]), ``count`` and ``next`` (int32
     [batch]) receive the result.  ``temperature``: a number for all, or one for each sequence
     (host); ``workspace``: a tensor of dv_verify_bytes bytes."""
     n, p, batch = _lengths("q_len", q_len)
