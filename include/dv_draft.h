@@ -97,8 +97,9 @@ DV_API int dv_verify_bytes(const int32_t* q_len, const dv_verify_args* a, uint64
  * infinite ones share all probability.  Draft 0 is there whatever its parent; any other
  * with a token outside [0, vocab), or that is not there, is passed over.  drawn[i][x]
  * counts as 0 where it is negative or NaN.  A row whose logits are all -infinity accepts
- * nothing; next is then -1.  A number outside [0, 1) counts as the nearest end (1: the
- * last token that r holds), NaN as 1.
+ * nothing; next is then -1.  A probability below 2^-1020 of the row's largest counts as 0.
+ * A number outside [0, 1) counts as the nearest end (1: the last token that r holds), NaN
+ * as 1.
  * A sequence without drafts gets count 0 and its next is left as it is.
  * temperature: host [batch], finite, 0 or more; NULL: all 1.  What the call writes
  * must not overlap what it reads nor each other.

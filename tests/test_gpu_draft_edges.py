@@ -197,6 +197,15 @@ def test_results_in_pinned_memory_and_none_in_pageable():
         draft.dv_verify(q_len, ints, token, x, u, *r, workspace=room)
     torch.cuda.synchronize()
     assert all(torch.equal(y.cpu(), z) for y, z in zip(a, b))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        draft.dv_verify(q_len, ints, token, x, u, *b, workspace=room)
+    for _ in range(3):
+        u.copy_(torch.rand(rows, device="cuda"))
+        graph.replay()
+        draft.dv_verify(q_len, ints, token, x, u, *a, workspace=room)
+        torch.cuda.synchronize()
+        assert torch.equal(a[1].cpu(), b[1]) and torch.equal(a[2].cpu(), b[2])
     with pytest.raises(dv.DvError, match=r"\(path, count, next: not in"):
         draft.dv_verify(q_len, ints, token, x, u, *host, workspace=room)
     torch.cuda.synchronize()
@@ -260,3 +269,26 @@ def test_nan_of_every_kind(dtype, nans, drawn):
                            temperature=np.array([rng.choice([0.0, 0.8])], np.float32))
         for _ in range(4):
             run_clear(draws())
+
+
+@pytest.mark.parametrize("drawn", [False, True])
+def test_probabilities_that_count_as_none(drawn):
+    """Below 2^-1020 of the largest (e^-707) a token is not there; above it is."""
+    V, T = 3000, np.full(2, 0.125, np.float32)
+    x = torch.full((4, V), -np.inf)
+    x[:, 100] = 0.0
+    x[:, 2500] = -706 * 0.125
+    x[:, 2900] = -708 * 0.125
+    q = torch.zeros((4, V))
+    q[:, 100] = 0.5
+    ints = torch.tensor([-1, 0, -1, 0], dtype=torch.int32).cuda()
+    path, count, follow = (torch.full((n,), -7, dtype=torch.int32, device="cuda") for n in (4, 2, 2))
+    for kind in TYPES.values():
+        logits = x.to(kind).cuda()
+        room = torch.empty(draft.dv_verify_bytes([2, 2], logits, drawn), dtype=torch.uint8,
+                           device="cuda")
+        # a guess of either with the number 0, which any probability is above
+        draft.dv_verify([2, 2], ints, torch.tensor([0, 2500, 0, 2900], dtype=torch.int32).cuda(),
+                        logits, torch.tensor([1.0, 0.0, 1.0, 0.0], device="cuda"), path, count,
+                        follow, temperature=T, drawn=q.cuda() if drawn else None, workspace=room)
+        assert count.tolist() == [2, 1] and follow.tolist() == [2500, 2500]
